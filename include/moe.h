@@ -110,8 +110,25 @@ typedef enum moe_ws_kind {
   MOE_WS_FFN = 2,
   MOE_WS_LAYER = 3,
   MOE_WS_FFN_BWD = 4,
-  MOE_WS_LAYER_BWD = 5
+  MOE_WS_LAYER_BWD = 5,
+  MOE_WS_MX_FFN = 6,        /* moe_mx_grouped_ffn; needs d and F to be multiples of 32 */
+  MOE_WS_DECODE = 7         /* moe_layer_decode; needs T <= MOE_DECODE_MAX_TOKENS      */
 } moe_ws_kind_t;
+
+/* Block-scaled ("MX", OCP microscaling) formats.  A [rows, cols] tensor, cols a multiple of 32, is
+ * held as elements and scales: 32 neighbouring values of a row share one power of two.
+ *    elements   [rows, cols / 2] bytes (E2M1: value 2i of a row in the low half of byte i) or
+ *               [rows, cols] bytes (E4M3, the finite-only encoding of 8-bit floats);
+ *               16-byte aligned
+ *    scales     [rows, cols / 32] bytes: s stands for 2^(s - 127), 255 for NaN; any alignment
+ * value = element * 2^(s - 127). */
+typedef enum moe_mx_format {
+  MOE_MX_E2M1 = 0,          /* 4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives  */
+  MOE_MX_E4M3 = 1           /* 8 bits: up to 448, steps of 2^-9 near zero               */
+} moe_mx_format_t;
+
+/* Tokens that moe_layer_decode takes at most. */
+#define MOE_DECODE_MAX_TOKENS 64
 
 /* Named regions inside a MOE_WS_LAYER workspace (moe_workspace_offset). */
 typedef enum moe_ws_region {
@@ -338,6 +355,76 @@ typedef enum moe_step {
 int moe_layer_forward_traced(const moe_shape_t* shape, const void* x, const void* w_router, const float* bias,
                              const void* w13, const void* w2, const void* ws13, const void* ws2,
                              void* out, void* ws, size_t ws_bytes, void* const* events, void* stream);
+
+/* Rows into a block-scaled format and back.
+ * moe_mx_quantize: for the 32 values v of a block, largest magnitude m,
+ *     s = clamp(floor(log2 m) - e, -127, 127) + 127,  e = 2 (E2M1) or 8 (E4M3);  s = 0 for m = 0,
+ *     element = v / 2^(s - 127) rounded to nearest, ties to even, cut at the format's largest value.
+ *   A block with an Inf or a NaN gets s = 255 (every value of it reads as NaN) and zero elements.
+ *   x [rows, cols] bf16.  Every byte of the elements and scales is written.
+ * moe_mx_dequantize: x = element * 2^(s - 127), rounded to nearest even where bf16 has fewer bits.
+ * rows >= 0 (0 is a no-op), cols a positive multiple of 32, rows * cols < 2^40. */
+int moe_mx_quantize(int64_t rows, int32_t cols, int format, const void* x, void* elements, void* scales,
+                    void* stream);
+int moe_mx_dequantize(int64_t rows, int32_t cols, int format, const void* elements, const void* scales, void* x,
+                      void* stream);
+
+/* Grouped SwiGLU expert MLP on block-scaled operands: moe_grouped_ffn with the rows in `format`
+ * and the weights in E2M1,
+ *     y_perm[r] = W2_e Q(silu(W1_e x_perm[r]) * (W3_e x_perm[r])),
+ * Q the activation in `format` too (moe_mx_quantize of the float32 values; the workspace holds it).
+ * Products and sums of each block are taken by the matrix cores on the elements, times both scales,
+ * accumulated in float32.
+ *    x_q, x_scales      [cap, d]             rows in expert order, in `format`
+ *    w13_q, w13_scales  [E_local * 2F, d]    E2M1, the rows as in w13
+ *    w2_q, w2_scales    [E_local * d, F]     E2M1, the rows as in w2
+ *    y_perm             [cap, d] bf16; rows outside every segment are not written
+ * Limits beside moe_grouped_ffn's: d and F multiples of 32.  Offsets, layouts and clamping as there.
+ * ws: MOE_WS_MX_FFN bytes. */
+int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, const void* x_scales,
+                       const int32_t* offsets, const void* w13_q, const void* w13_scales, const void* w2_q,
+                       const void* w2_scales, void* y_perm, void* ws, size_t ws_bytes, void* stream);
+
+/* Residual addition and RMS norm in front of a layer, row by row:
+ *     h = bf16(x + residual),  rstd = 1 / sqrt(mean(h^2) + eps),  y = bf16(h * rstd * gamma),
+ *     (y_q, y_scales) = moe_mx_quantize(y) in E4M3,
+ * statistics in float32.  x, residual, h, y [rows, d] bf16; gamma [d] bf16; rstd [rows] f32;
+ * y_q, y_scales [rows, d] in E4M3.
+ *   residual NULL: h is x itself, nothing is added and h must be NULL.  Otherwise h is required; it
+ *                  may be x's or residual's own buffer.
+ *   y, or y_q and y_scales together, may be NULL (not wanted), not all three; rstd may be NULL.
+ *   eps >= 0 and finite.  A row of zeros with eps = 0 gives NaN.
+ * No output but h may overlap an input.  d a multiple of 8, of 32 where y_q is given; rows >= 0. */
+int moe_add_rmsnorm(int64_t rows, int32_t d, float eps, const void* x, const void* residual, const void* gamma,
+                    void* h, void* y, void* y_q, void* y_scales, float* rstd, void* stream);
+
+/* Backward of moe_add_rmsnorm, for the gradient dy of y and, where h goes on as the residual
+ * stream, the gradient dh that comes back to it (NULL = none).  With u = h * rstd, g = dy * gamma:
+ *     dx = bf16(rstd * (g - u * mean(g * u)) + dh)     the gradient of x and of residual alike
+ *     dgamma = bf16(sum over rows of dy * u)           summed in float32 in a fixed order
+ * h and rstd are the forward's (h = x where it had no residual).  dx may be dy's or dh's own buffer.
+ * rows = 0 gives dgamma = 0.  ws: moe_add_rmsnorm_workspace_size bytes. */
+int moe_add_rmsnorm_backward(int64_t rows, int32_t d, const void* dy, const void* dh, const void* h,
+                             const void* gamma, const float* rstd, void* dx, void* dgamma, void* ws,
+                             size_t ws_bytes, void* stream);
+/* Bytes of workspace of moe_add_rmsnorm_backward (0 for invalid sizes; moe_last_error() says why). */
+size_t moe_add_rmsnorm_workspace_size(int64_t rows, int32_t d);
+
+/* The whole layer for a few tokens (T <= MOE_DECODE_MAX_TOKENS), by kernels that stream each active
+ * expert's weights once: moe_layer_forward's result, up to the order of float32 sums and without the
+ * rounding of the expert rows before the combine,
+ *     out[t] = bf16( sum over the kept local slots of topk_w * W2 bf16(silu(W1 x) * (W3 x)) + shared ).
+ * The weights are bf16 (every *_scales NULL) or E2M1 (every one given): then w13, w2, ws13 and ws2 are
+ * the elements, their values enter the products exactly, and x and the activation stay bf16.  Either
+ * way the router and x are bf16.  Honours expert_capacity; ignores fusion.
+ * E2M1 needs d, F and F_shared to be multiples of 32.  The chosen experts and their gates are left at
+ * the start of the workspace, at the offsets moe_workspace_offset gives for MOE_REGION_TOPK_IDX and
+ * MOE_REGION_TOPK_W.  Deterministic.  Calls that may overlap need a workspace each.
+ * ws: MOE_WS_DECODE bytes. */
+int moe_layer_decode(const moe_shape_t* shape, const void* x, const void* w_router, const float* bias,
+                     const void* w13, const void* w13_scales, const void* w2, const void* w2_scales,
+                     const void* ws13, const void* ws13_scales, const void* ws2, const void* ws2_scales,
+                     void* out, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

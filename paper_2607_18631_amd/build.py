@@ -22,8 +22,8 @@ PROBE_SRC = os.path.join(HERE, "probe", "stream.hip")
 PROBE_LIB = os.path.join(HERE, "libmoe_probe.so")
 ARCH = "gfx950"
 
-SOURCES = ["api.cpp", "sizes.cpp", "gemm.hip", "gemm_phase.hip", "gemm_bwd.hip", "route.hip", "permute.hip", "combine.hip",
-           "layer_bwd.hip"]
+SOURCES = ["api.cpp", "api_serving.cpp", "sizes.cpp", "gemm.hip", "gemm_phase.hip", "gemm_bwd.hip", "route.hip", "permute.hip", "combine.hip",
+           "layer_bwd.hip", "norm_mx.hip", "mx_gemm.hip", "decode.hip"]
 
 FLAGS = [f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          # keep the compiler from emitting packed fp32 VALU ops (v_pk_*_f32)

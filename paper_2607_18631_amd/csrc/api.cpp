@@ -10,11 +10,13 @@
 #include <string>
 
 #include "../../include/moe.h"
+#include "api_common.hpp"
 #include "kernels.hpp"
 
-namespace {
+namespace moe {
+namespace abi {
 
-thread_local std::string g_err;
+static thread_local std::string g_err;
 
 int fail(int status, const char* fmt, ...) {
   char buf[512];
@@ -31,15 +33,19 @@ int ok() {
   return MOE_OK;
 }
 
-constexpr size_t kAlign = 256;
-size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
-
 // rows of the expert-ordered buffers: every local slot (offsets layout) or E_local equal
 // segments of expert_capacity rows (masked-decode layout)
 int64_t capacity(const moe_shape_t* s) {
   if (s->expert_capacity > 0) return (int64_t)s->E_local * s->expert_capacity;
   return s->T * (int64_t)(s->top_k < s->E_local ? s->top_k : s->E_local);
 }
+
+}  // namespace abi
+}  // namespace moe
+
+namespace {
+
+using namespace moe::abi;
 
 // Expected rows per local expert of a layer call (tile-shape choice only; the real counts stay
 // on the device): T * top_k / E under uniform routing, at most the expert capacity in the masked
@@ -51,7 +57,9 @@ int64_t expected_rows(const moe_shape_t* s) {
   return r;
 }
 
-int check_shape(const moe_shape_t* s) {
+}  // namespace
+
+int moe::abi::check_shape(const moe_shape_t* s) {
   if (!s) return fail(MOE_ERR_INVALID_ARG, "shape is NULL");
   if (s->T < 0) return fail(MOE_ERR_INVALID_ARG, "T (%lld) < 0", (long long)s->T);
   if (s->d <= 0) return fail(MOE_ERR_INVALID_ARG, "d (%d) <= 0", s->d);
@@ -96,6 +104,8 @@ int check_shape(const moe_shape_t* s) {
   return MOE_OK;
 }
 
+namespace {
+
 // the up-projection reads token rows through row_token (per-lane 32-bit offsets into x)
 bool gather_fits(const moe_shape_t* s) { return s->T * (int64_t)s->d * 2 < (int64_t(1) << 32); }
 bool fuse_gather(const moe_shape_t* s) {
@@ -104,18 +114,16 @@ bool fuse_gather(const moe_shape_t* s) {
 bool fuse_combine(const moe_shape_t* s) { return (s->fusion & MOE_FUSE_COMBINE) != 0;
 }
 
-int check_ptr(const void* p, size_t align, const char* name) {
+}  // namespace
+
+int moe::abi::check_ptr(const void* p, size_t align, const char* name) {
   if (!p) return fail(MOE_ERR_INVALID_ARG, "%s is NULL", name);
   if (reinterpret_cast<uintptr_t>(p) % align)
     return fail(MOE_ERR_INVALID_ARG, "%s (%p) is not %zu-byte aligned", name, p, align);
   return MOE_OK;
 }
 
-#define CHECK(expr)          \
-  do {                       \
-    int _st = (expr);        \
-    if (_st != MOE_OK) return _st; \
-  } while (0)
+namespace {
 
 // ---- workspace layouts ----
 // router logits: one [T, E] fp32 partial per K chunk of the logits GEMM
@@ -218,12 +226,15 @@ size_t ws_need(const moe_shape_t* s, int kind) {
     case MOE_WS_LAYER: return layer_layout(s).total;
     case MOE_WS_FFN_BWD: return ws_ffn_bwd(s);
     case MOE_WS_LAYER_BWD: return layer_bwd_layout(s).total;
+    case MOE_WS_MX_FFN: return mx_ffn_layout(s).total;
+    case MOE_WS_DECODE: return decode_layout(s).total;
     default: return 0;
   }
 }
 
-int check_ws(const moe_shape_t* s, int kind, const void* ws, size_t ws_bytes) {
-  const size_t need = ws_need(s, kind);
+}  // namespace
+
+int moe::abi::check_ws_bytes(size_t need, const void* ws, size_t ws_bytes) {
   if (need == 0) return MOE_OK;
   if (!ws) return fail(MOE_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", need);
   if (reinterpret_cast<uintptr_t>(ws) % kAlign)
@@ -232,14 +243,16 @@ int check_ws(const moe_shape_t* s, int kind, const void* ws, size_t ws_bytes) {
   return MOE_OK;
 }
 
-int hip_status(hipError_t e, const char* what) {
+int moe::abi::hip_status(hipError_t e, const char* what) {
   if (e == hipSuccess) return MOE_OK;
   return fail(MOE_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
-template <class T>
-inline T* at(void* base, size_t off) { return reinterpret_cast<T*>(static_cast<char*>(base) + off); }
+namespace {
+
+int check_ws(const moe_shape_t* s, int kind, const void* ws, size_t ws_bytes) {
+  return check_ws_bytes(ws_need(s, kind), ws, ws_bytes);
+}
 
 // ---- dispatch (arguments already validated) ----
 using Marker = int (*)(int step);
@@ -573,10 +586,12 @@ const char* moe_last_error(void) { return g_err.c_str(); }
 
 size_t moe_workspace_size(const moe_shape_t* shape, int kind) {
   if (check_shape(shape) != MOE_OK) return 0;
-  if (kind < MOE_WS_ROUTE || kind > MOE_WS_LAYER_BWD) {
+  if (kind < MOE_WS_ROUTE || kind > MOE_WS_DECODE) {
     fail(MOE_ERR_INVALID_ARG, "workspace kind (%d) unknown", kind);
     return 0;
   }
+  if (kind == MOE_WS_MX_FFN && check_mx_shape(shape) != MOE_OK) return 0;
+  if (kind == MOE_WS_DECODE && check_decode_shape(shape) != MOE_OK) return 0;
   size_t n = ws_need(shape, kind);
   return n ? n : kAlign;
 }

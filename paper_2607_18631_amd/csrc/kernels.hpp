@@ -258,4 +258,100 @@ hipError_t launch_zero_f32(float* acc, int64_t n, hipStream_t stream);
 // out[i] = bf16(acc[i]) for i < n, n % 8 == 0
 hipError_t launch_round_bf16(const float* acc, bf16_t* out, int64_t n, hipStream_t stream);
 
+// ---- block-scaled formats, the norm in front of the layer, the few-token layer ----
+enum MxFormat { MX_E2M1 = 0, MX_E4M3 = 1 };
+
+// n values (n % 32 == 0), rows being whole blocks: elements and one scale byte per 32 values
+struct MxConvertProblem {
+  const bf16_t* x;            // quantize: in
+  bf16_t* out;                // dequantize: out
+  uint8_t* elements;
+  uint8_t* scales;
+  int64_t n;
+  int32_t format;
+};
+hipError_t launch_mx_quantize(const MxConvertProblem& p, hipStream_t stream);
+hipError_t launch_mx_dequantize(const MxConvertProblem& p, hipStream_t stream);
+
+struct AddNormProblem {
+  const bf16_t* x;            // [rows, d]
+  const bf16_t* residual;     // [rows, d] or nullptr
+  const bf16_t* gamma;        // [d]
+  bf16_t* h;                  // [rows, d], with residual
+  bf16_t* y;                  // [rows, d] or nullptr
+  uint8_t* y_q;               // [rows, d] e4m3 or nullptr
+  uint8_t* y_scales;          // [rows, d / 32], with y_q
+  float* rstd;                // [rows] or nullptr
+  int64_t rows;
+  int32_t d;
+  float eps;
+};
+hipError_t launch_add_norm(const AddNormProblem& p, hipStream_t stream);
+
+struct AddNormBwdProblem {
+  const bf16_t* dy;           // [rows, d]
+  const bf16_t* dh;           // [rows, d] or nullptr
+  const bf16_t* h;            // [rows, d]
+  const bf16_t* gamma;        // [d]
+  const float* rstd;          // [rows]
+  bf16_t* dx;                 // [rows, d]
+  bf16_t* dgamma;             // [d]
+  float* parts;               // workspace [add_norm_bwd_parts(rows, d), d]
+  int64_t rows;
+  int32_t d;
+};
+// partial sums of dgamma: one row of d floats per workgroup of the first kernel
+int add_norm_bwd_parts(int64_t rows, int d);
+hipError_t launch_add_norm_bwd(const AddNormBwdProblem& p, hipStream_t stream);
+
+// One grouped product on block-scaled operands: Y[r, n] = sum_k X[r, k] W_g[n, k], X in `format`,
+// W in e2m1, K % 32 == 0, N % 32 == 0.
+//   swiglu: W_g holds 2N rows (gate, then up); Y is the activation in `format` (elements, scales)
+//   else    Y is bf16
+struct MxGemmProblem {
+  const uint8_t* X;           // [rows, K] elements
+  const uint8_t* X_scales;    // [rows, K / 32]
+  const int32_t* offsets;     // as in GemmProblem
+  int32_t groups;
+  int64_t max_rows;
+  int32_t seg_stride;
+  const uint8_t* W;           // elements of all groups, (swiglu ? 2N : N) rows each
+  const uint8_t* W_scales;
+  int32_t N, K;
+  int32_t format;
+  bool swiglu;
+  bf16_t* Y;                  // bf16 result [rows, N]
+  uint8_t* Yq;                // swiglu: elements [rows, N]
+  uint8_t* Y_scales;          // swiglu: scales [rows, N / 32]
+};
+hipError_t launch_mx_gemm(const MxGemmProblem& p, hipStream_t stream);
+
+// Few-token layer: at most kDecodeTokens tokens, so the tokens of an expert are a 64-bit mask.
+constexpr int kDecodeTokens = 64;
+constexpr int kDecodeSlots = kDecodeTokens * 16;
+// The experts that have rows, written by the kernels: expert a of n_active owns the slots (token *
+// top_k + choice, ascending token) slot[begin[a]] .. slot[begin[a + 1] - 1].
+struct DecodePlan {
+  int32_t n_active;
+  int32_t expert[kDecodeSlots];
+  int32_t begin[kDecodeSlots + 1];
+  int32_t slot[kDecodeSlots];
+};
+// K chunks of the router logits
+int decode_logits_splits(int E, int d);
+struct DecodeProblem {
+  const bf16_t* x;            // [T, d]
+  const bf16_t* w_router;     // [E, d]
+  GateProblem gate;           // logits partials, topk_idx, topk_w
+  float* logits;              // [splits, T, E]
+  DecodePlan* plan;
+  const void *w13, *w2, *ws13, *ws2;      // bf16, or e2m1 elements where the scales are set
+  const uint8_t *w13_scales, *w2_scales, *ws13_scales, *ws2_scales;
+  bf16_t* act;                // [T * top_k, F], row = slot
+  bf16_t* act_shared;         // [T, F_shared]
+  bf16_t* out;                // [T, d]
+  int32_t T, d, E, top_k, e_begin, E_local, F, F_shared, expert_capacity;
+};
+hipError_t launch_decode(const DecodeProblem& p, hipStream_t stream);
+
 }  // namespace moe

@@ -51,4 +51,21 @@ PermuteWs permute_ws(int64_t T, int E_local) {
   return w;
 }
 
+// Few-token layer: one wave multiplies 16 experts by a chunk of K for all tokens; chunks of at least
+// 256 values, at most 16 of them (the gate adds the partials).
+int decode_logits_splits(int E, int d) {
+  (void)E;
+  const int s = (d + 255) / 256;
+  return s < 16 ? s : 16;
+}
+
+// Norm backward: every workgroup leaves one row of partial sums of dgamma.  Four workgroups per
+// compute unit of an MI355X at most, and at least 4 rows for each of its four waves.
+int add_norm_bwd_parts(int64_t rows, int d) {
+  (void)d;
+  int64_t n = (rows + 15) / 16;
+  n = n < 1024 ? n : 1024;
+  return (int)(n > 1 ? n : 1);
+}
+
 }  // namespace moe

@@ -18,7 +18,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libmoe_mi355x.so")
 
 MOE_OK, MOE_ERR_INVALID_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP = range(5)
-MOE_WS_ROUTE, MOE_WS_PERMUTE, MOE_WS_FFN, MOE_WS_LAYER, MOE_WS_FFN_BWD, MOE_WS_LAYER_BWD = range(6)
+(MOE_WS_ROUTE, MOE_WS_PERMUTE, MOE_WS_FFN, MOE_WS_LAYER, MOE_WS_FFN_BWD, MOE_WS_LAYER_BWD, MOE_WS_MX_FFN,
+ MOE_WS_DECODE) = range(8)
+MOE_MX_E2M1, MOE_MX_E4M3 = range(2)
+MOE_DECODE_MAX_TOKENS = 64
 MOE_FUSION_SET, MOE_FUSE_GATHER, MOE_FUSE_COMBINE = 0x10, 0x1, 0x2
 (MOE_REGION_TOPK_IDX, MOE_REGION_TOPK_W, MOE_REGION_COUNTS, MOE_REGION_OFFSETS, MOE_REGION_ROW_TOKEN,
  MOE_REGION_SLOT_ROW, MOE_REGION_X_PERM, MOE_REGION_Y_PERM, MOE_REGION_SHARED_Y) = range(9)
@@ -26,7 +29,8 @@ MOE_FUSION_SET, MOE_FUSE_GATHER, MOE_FUSE_COMBINE = 0x10, 0x1, 0x2
 EXPORTS = ["moe_abi_version", "moe_status_string", "moe_last_error", "moe_workspace_size",
            "moe_workspace_offset", "moe_route", "moe_permute", "moe_grouped_ffn", "moe_combine",
            "moe_layer_forward", "moe_layer_forward_traced", "moe_grouped_ffn_backward", "moe_layer_backward",
-           "moe_permute_noalloc"]
+           "moe_permute_noalloc", "moe_mx_quantize", "moe_mx_dequantize", "moe_mx_grouped_ffn", "moe_add_rmsnorm",
+           "moe_add_rmsnorm_backward", "moe_add_rmsnorm_workspace_size", "moe_layer_decode"]
 MOE_STEP_NAMES = ["router_gemm", "gate", "histogram", "permute", "ffn_up", "ffn_down", "shared_up",
                   "shared_down", "combine"]
 
@@ -83,8 +87,19 @@ def lib():
         L.moe_layer_forward.argtypes = [sp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
         L.moe_layer_forward_traced.argtypes = [sp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t,
                                                ctypes.POINTER(_vp), _vp]
+        sz, i32, i64, f32 = ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+        L.moe_mx_quantize.argtypes = [i64, i32, i32, _vp, _vp, _vp, _vp]
+        L.moe_mx_dequantize.argtypes = [i64, i32, i32, _vp, _vp, _vp, _vp]
+        L.moe_mx_grouped_ffn.argtypes = [sp, i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp]
+        L.moe_add_rmsnorm.argtypes = [i64, i32, f32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+        L.moe_add_rmsnorm_backward.argtypes = [i64, i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp]
+        L.moe_add_rmsnorm_workspace_size.argtypes = [i64, i32]
+        L.moe_add_rmsnorm_workspace_size.restype = sz
+        L.moe_layer_decode.argtypes = [sp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp]
         for f in ("moe_route", "moe_permute", "moe_grouped_ffn", "moe_combine", "moe_layer_forward",
-                  "moe_layer_forward_traced", "moe_grouped_ffn_backward", "moe_layer_backward"):
+                  "moe_layer_forward_traced", "moe_grouped_ffn_backward", "moe_layer_backward", "moe_mx_quantize",
+                  "moe_mx_dequantize", "moe_mx_grouped_ffn", "moe_add_rmsnorm", "moe_add_rmsnorm_backward",
+                  "moe_layer_decode"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -191,6 +206,165 @@ def moe_layer_forward_traced(sh, x, w_router, bias, w13, w2, ws13, ws2, out, ws,
 
 
 # ---------------------------------------------------------------------------------------
+# block-scaled formats, the norm in front of a layer, the few-token layer
+#
+# These calls check their tensors (dtype, shape, contiguity, one device) before the library sees
+# pointers, and run on the tensors' device, by default on its current stream.
+# ---------------------------------------------------------------------------------------
+def _refuse(message: str):
+    raise MoEError(MOE_ERR_INVALID_ARG, message)
+
+
+def _take(device, name, t, dtype, *shape):
+    """Pointer of a tensor that has to have this dtype and shape on this device."""
+    if t is None:
+        _refuse(f"{name} is missing")
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; "
+                f"expected contiguous {dtype} {shape} on {device}")
+    return t.data_ptr()
+
+
+def _on(device, stream, call, *args):
+    """Runs a library call on ``device`` and ``stream`` (None: that device's current stream)."""
+    import torch
+    if device.type != "cuda":
+        _refuse(f"tensors are on {device}, not on a GPU")
+    if stream is None:
+        stream = torch.cuda.current_stream(device).cuda_stream
+    if device.index == torch.cuda.current_device():
+        _check(call(*args, stream))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, stream))
+
+
+def _matrix(name, t):
+    if t.dim() != 2:
+        _refuse(f"{name} has {t.dim()} dimensions, expected 2")
+    return t.shape
+
+
+def mx_elements_per_row(format: int, cols: int) -> int:
+    """Bytes of one row's elements in a block-scaled format."""
+    return cols // 2 if format == MOE_MX_E2M1 else cols
+
+
+def moe_mx_quantize(format, x, elements, scales, stream=None):
+    """bf16 ``x [rows, cols]`` into uint8 ``elements [rows, cols / 2 or cols]`` and ``scales [rows, cols / 32]``."""
+    import torch
+    rows, cols = _matrix("x", x)
+    dev, u8 = x.device, torch.uint8
+    _on(dev, stream, lib().moe_mx_quantize, rows, cols, format, _take(dev, "x", x, torch.bfloat16, rows, cols),
+        _take(dev, "elements", elements, u8, rows, mx_elements_per_row(format, cols)),
+        _take(dev, "scales", scales, u8, rows, cols // 32))
+
+
+def moe_mx_dequantize(format, elements, scales, x, stream=None):
+    """The values of block-scaled ``elements`` and ``scales`` into bf16 ``x [rows, cols]``."""
+    import torch
+    rows, cols = _matrix("x", x)
+    dev, u8 = x.device, torch.uint8
+    _on(dev, stream, lib().moe_mx_dequantize, rows, cols, format,
+        _take(dev, "elements", elements, u8, rows, mx_elements_per_row(format, cols)),
+        _take(dev, "scales", scales, u8, rows, cols // 32), _take(dev, "x", x, torch.bfloat16, rows, cols))
+
+
+def _bytes(device, name, t, n):
+    """Pointer of a contiguous uint8 tensor of at least n values (any shape)."""
+    import torch
+    if t is None:
+        _refuse(f"{name} is missing")
+    if t.dtype is not torch.uint8 or t.numel() < n or t.device != device or not t.is_contiguous():
+        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; "
+                f"expected {n} contiguous uint8 values on {device}")
+    return t.data_ptr()
+
+
+def _ws(device, ws):
+    """(pointer, bytes) of a workspace."""
+    if ws is None:
+        return None, 0
+    return _bytes(device, "ws", ws, 0), ws.numel()
+
+
+def moe_mx_grouped_ffn(sh, format, x_q, x_scales, offsets, w13_q, w13_scales, w2_q, w2_scales, y_perm, ws, stream=None):
+    """``x_q`` / ``x_scales`` and ``y_perm`` have ``sh.capacity`` rows."""
+    import torch
+    dev, d, F, El = x_q.device, sh.d, sh.F, sh.E_local
+    cap = sh.capacity
+    _on(dev, stream, lib().moe_mx_grouped_ffn, ctypes.byref(shape_c(sh)), format,
+        _bytes(dev, "x_q", x_q, cap * mx_elements_per_row(format, d)), _bytes(dev, "x_scales", x_scales, cap * (d // 32)),
+        _take(dev, "offsets", offsets, torch.int32, El if sh.expert_capacity > 0 else El + 1),
+        _bytes(dev, "w13_q", w13_q, El * 2 * F * d // 2), _bytes(dev, "w13_scales", w13_scales, El * 2 * F * (d // 32)),
+        _bytes(dev, "w2_q", w2_q, El * d * F // 2), _bytes(dev, "w2_scales", w2_scales, El * d * (F // 32)),
+        _take(dev, "y_perm", y_perm, torch.bfloat16, cap, d), *_ws(dev, ws))
+
+
+def moe_add_rmsnorm(x, residual, gamma, eps, h, y, y_q=None, y_scales=None, rstd=None, stream=None):
+    import torch
+    rows, d = _matrix("x", x)
+    dev, bf, u8 = x.device, torch.bfloat16, torch.uint8
+
+    def opt(name, t, dtype, *shape):
+        return None if t is None else _take(dev, name, t, dtype, *shape)
+
+    _on(dev, stream, lib().moe_add_rmsnorm, rows, d, eps, _take(dev, "x", x, bf, rows, d),
+        opt("residual", residual, bf, rows, d), _take(dev, "gamma", gamma, bf, d), opt("h", h, bf, rows, d),
+        opt("y", y, bf, rows, d), opt("y_q", y_q, u8, rows, d), opt("y_scales", y_scales, u8, rows, d // 32),
+        opt("rstd", rstd, torch.float32, rows))
+
+
+def moe_add_rmsnorm_backward(dy, dh, h, gamma, rstd, dx, dgamma, ws, stream=None):
+    import torch
+    rows, d = _matrix("dy", dy)
+    dev, bf = dy.device, torch.bfloat16
+    _on(dev, stream, lib().moe_add_rmsnorm_backward, rows, d, _take(dev, "dy", dy, bf, rows, d),
+        None if dh is None else _take(dev, "dh", dh, bf, rows, d), _take(dev, "h", h, bf, rows, d),
+        _take(dev, "gamma", gamma, bf, d), _take(dev, "rstd", rstd, torch.float32, rows),
+        _take(dev, "dx", dx, bf, rows, d), _take(dev, "dgamma", dgamma, bf, d), *_ws(dev, ws))
+
+
+def add_rmsnorm_workspace_size(rows: int, d: int) -> int:
+    n = lib().moe_add_rmsnorm_workspace_size(rows, d)
+    if n == 0:
+        raise MoEError(MOE_ERR_INVALID_ARG, last_error())
+    return n
+
+
+def alloc_add_rmsnorm_workspace(rows: int, d: int, device="cuda"):
+    import torch
+    return torch.empty(add_rmsnorm_workspace_size(rows, d), dtype=torch.uint8, device=device)
+
+
+def moe_layer_decode(sh, x, w_router, bias, w13, w2, ws13, ws2, out, ws, scales=None, stream=None):
+    """``scales``: None with bf16 weights, or (w13_scales, w2_scales, ws13_scales, ws2_scales) with e2m1 ones
+    (the last two None without a shared expert)."""
+    import torch
+    dev, bf = x.device, torch.bfloat16
+    T, d, F, Fs, El = sh.T, sh.d, sh.F, sh.F_shared, sh.E_local
+
+    def weights(name, t, s, rows, K):
+        if t is None:
+            _refuse(f"{name} is missing")
+        if scales is None:
+            if t.dtype is not bf or t.numel() != rows * K or t.device != dev or not t.is_contiguous():
+                _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}; expected {rows * K} contiguous {bf} "
+                        f"values on {dev}")
+            return t.data_ptr(), None
+        return _bytes(dev, name, t, rows * K // 2), _bytes(dev, name + "_scales", s, rows * (K // 32))
+
+    s = scales if scales is not None else (None,) * 4
+    none = (None, None)
+    _on(dev, stream, lib().moe_layer_decode, ctypes.byref(shape_c(sh)), _take(dev, "x", x, bf, T, d),
+        _take(dev, "w_router", w_router, bf, sh.E, d),
+        None if bias is None else _take(dev, "bias", bias, torch.float32, sh.E),
+        *weights("w13", w13, s[0], El * 2 * F, d), *weights("w2", w2, s[1], El * d, F),
+        *(weights("ws13", ws13, s[2], 2 * Fs, d) if Fs else none), *(weights("ws2", ws2, s[3], d, Fs) if Fs else none),
+        _take(dev, "out", out, bf, T, d), *_ws(dev, ws))
+
+
+# ---------------------------------------------------------------------------------------
 # device placement helpers (torch is plumbing: memory and streams)
 # ---------------------------------------------------------------------------------------
 def to_device_bf16(bits: np.ndarray, device="cuda"):
@@ -255,6 +429,31 @@ class DeviceLayer:
                            self.ws, g["dx"], g["dw_router"], g["dw13"], g["dw2"], g["dws13"], g["dws2"],
                            self.ws_bwd, stream)
         return g
+
+    def quantize(self):
+        """The expert weights in e2m1 for ``decode(mx=True)``: per tensor (elements, scales)."""
+        import torch
+        self.mx = {}
+        for name in ("w13", "w2", "ws13", "ws2"):
+            w = getattr(self, name)
+            if w is not None:
+                rows, cols = w.numel() // w.shape[-1], w.shape[-1]
+                q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=self.device)
+                s = torch.empty((rows, cols // 32), dtype=torch.uint8, device=self.device)
+                moe_mx_quantize(MOE_MX_E2M1, w.view(rows, cols), q, s)
+                self.mx[name] = (q, s)
+        return self.mx
+
+    def decode(self, mx: bool = False, stream=None):
+        """``moe_layer_decode`` with the layer's bf16 weights, or with the e2m1 ones of ``quantize()``."""
+        if getattr(self, "ws_decode", None) is None:
+            self.ws_decode = alloc_workspace(self.shape, MOE_WS_DECODE, self.device)
+        names = ("w13", "w2", "ws13", "ws2")
+        w, scales = [getattr(self, n) for n in names], None
+        if mx:
+            w, scales = zip(*(self.mx.get(n, (None, None)) for n in names))
+        moe_layer_decode(self.shape, self.x, self.w_router, self.bias, *w, self.out, self.ws_decode, scales, stream)
+        return self.out
 
     def region(self, region: int, dtype, shape):
         import torch
