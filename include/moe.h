@@ -118,10 +118,9 @@ typedef enum moe_ws_kind {
 /* Block-scaled ("MX", OCP microscaling) formats.  A [rows, cols] tensor, cols a multiple of 32, is
  * held as elements and scales: 32 neighbouring values of a row share one power of two.
  *    elements   [rows, cols / 2] bytes (E2M1: value 2i of a row in the low half of byte i) or
- *               [rows, cols] bytes (E4M3, the finite-only encoding of 8-bit floats);
- *               16-byte aligned
- *    scales     [rows, cols / 32] bytes: s stands for 2^(s - 127), 255 for NaN; any alignment
- * value = element * 2^(s - 127). */
+ *               [rows, cols] bytes (E4M3, the finite-only encoding of 8-bit floats)
+ *    scales     [rows, cols / 32] bytes: s stands for 2^(s - 127), 255 for NaN
+ * both 16-byte aligned; value = element * 2^(s - 127). */
 typedef enum moe_mx_format {
   MOE_MX_E2M1 = 0,          /* 4 bits: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives  */
   MOE_MX_E4M3 = 1           /* 8 bits: up to 448, steps of 2^-9 near zero               */
@@ -417,7 +416,7 @@ size_t moe_add_rmsnorm_workspace_size(int64_t rows, int32_t d);
  * The weights are bf16 (every *_scales NULL) or E2M1 (every one given): then w13, w2, ws13 and ws2 are
  * the elements, their values enter the products exactly, and x and the activation stay bf16.  Either
  * way the router and x are bf16.  Honours expert_capacity; ignores fusion.
- * E2M1 needs d, F and F_shared to be multiples of 32.  The chosen experts and their gates are left at
+ * d, F and F_shared are below 2^20; with E2M1 they are multiples of 32, d <= 16384 and F, F_shared <= 32768.  The chosen experts and their gates are left at
  * the start of the workspace, at the offsets moe_workspace_offset gives for MOE_REGION_TOPK_IDX and
  * MOE_REGION_TOPK_W.  Deterministic.  Calls that may overlap need a workspace each.
  * ws: MOE_WS_DECODE bytes. */

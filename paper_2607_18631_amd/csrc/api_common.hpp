@@ -35,6 +35,9 @@ inline int check_mx_shape(const moe_shape_t* s) {
 inline int check_decode_shape(const moe_shape_t* s) {
   if (s->T > MOE_DECODE_MAX_TOKENS)
     return fail(MOE_ERR_UNSUPPORTED, "T (%lld) > %d (MOE_DECODE_MAX_TOKENS)", (long long)s->T, MOE_DECODE_MAX_TOKENS);
+  // 32-bit byte offsets into 16 weight rows and into the activations of every slot
+  const int32_t widest = s->d > s->F ? (s->d > s->F_shared ? s->d : s->F_shared) : (s->F > s->F_shared ? s->F : s->F_shared);
+  if (widest >= (1 << 20)) return fail(MOE_ERR_UNSUPPORTED, "d, F or F_shared (%d) >= 2^20", widest);
   return MOE_OK;
 }
 
@@ -51,7 +54,7 @@ inline MxFfnLayout mx_ffn_layout(const moe_shape_t* s) {
 
 // MOE_WS_DECODE: the routing first, at the same offsets as in a MOE_WS_LAYER workspace
 struct DecodeLayout {
-  size_t topk_idx, topk_w, logits, plan, act, act_shared, total;
+  size_t topk_idx, topk_w, logits, plan, act, act_shared, y, total;
 };
 inline DecodeLayout decode_layout(const moe_shape_t* s) {
   DecodeLayout L{};
@@ -68,6 +71,7 @@ inline DecodeLayout decode_layout(const moe_shape_t* s) {
   L.plan = take(sizeof(DecodePlan));
   L.act = take(T * k * (size_t)s->F * 2);
   L.act_shared = take(T * (size_t)s->F_shared * 2);
+  L.y = take((T * k + (s->F_shared > 0 ? T : 0)) * (size_t)s->d * sizeof(float));
   L.total = off;
   return L;
 }

@@ -61,7 +61,7 @@ int moe_mx_quantize(int64_t rows, int32_t cols, int format, const void* x, void*
   if (rows == 0) return ok();
   CHECK(check_ptr(x, 16, "x"));
   CHECK(check_ptr(elements, 16, "elements"));
-  CHECK(check_ptr(scales, 1, "scales"));
+  CHECK(check_ptr(scales, 16, "scales"));
   CHECK(hip_status(moe::launch_mx_quantize(mx_problem(rows, cols, format, x, nullptr, elements, scales),
                                            as_stream(stream)),
                    "block-scaled conversion launch"));
@@ -73,7 +73,7 @@ int moe_mx_dequantize(int64_t rows, int32_t cols, int format, const void* elemen
   CHECK(check_mx_sizes(rows, cols, format));
   if (rows == 0) return ok();
   CHECK(check_ptr(elements, 16, "elements"));
-  CHECK(check_ptr(scales, 1, "scales"));
+  CHECK(check_ptr(scales, 16, "scales"));
   CHECK(check_ptr(x, 16, "x"));
   CHECK(hip_status(moe::launch_mx_dequantize(mx_problem(rows, cols, format, nullptr, x, elements, scales),
                                              as_stream(stream)),
@@ -91,12 +91,12 @@ int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, co
     return fail(MOE_ERR_UNSUPPORTED, "E_local (%d) > %d", shape->E_local, moe::kMaxGroups);
   if (shape->T == 0) return ok();
   CHECK(check_ptr(x_q, 16, "x_q"));
-  CHECK(check_ptr(x_scales, 1, "x_scales"));
+  CHECK(check_ptr(x_scales, 16, "x_scales"));
   CHECK(check_ptr(offsets, 4, "offsets"));
   CHECK(check_ptr(w13_q, 16, "w13_q"));
-  CHECK(check_ptr(w13_scales, 1, "w13_scales"));
+  CHECK(check_ptr(w13_scales, 16, "w13_scales"));
   CHECK(check_ptr(w2_q, 16, "w2_q"));
-  CHECK(check_ptr(w2_scales, 1, "w2_scales"));
+  CHECK(check_ptr(w2_scales, 16, "w2_scales"));
   CHECK(check_ptr(y_perm, 16, "y_perm"));
   const MxFfnLayout L = mx_ffn_layout(shape);
   CHECK(check_ws_bytes(L.total, ws, ws_bytes));
@@ -149,7 +149,10 @@ int moe_add_rmsnorm(int64_t rows, int32_t d, float eps, const void* x, const voi
   if (y) CHECK(check_ptr(y, 16, "y"));
   if ((y_q != nullptr) != (y_scales != nullptr))
     return fail(MOE_ERR_INVALID_ARG, "y_q and y_scales go together: %s is NULL", y_q ? "y_scales" : "y_q");
-  if (y_q) CHECK(check_ptr(y_q, 16, "y_q"));
+  if (y_q) {
+    CHECK(check_ptr(y_q, 16, "y_q"));
+    CHECK(check_ptr(y_scales, 16, "y_scales"));
+  }
   if (rstd) CHECK(check_ptr(rstd, 4, "rstd"));
   moe::AddNormProblem p{};
   p.x = static_cast<const moe::bf16_t*>(x);
@@ -218,6 +221,10 @@ int moe_layer_decode(const moe_shape_t* shape, const void* x, const void* w_rout
     CHECK(check_mx_shape(s));
     if (s->F_shared % 32)
       return fail(MOE_ERR_UNSUPPORTED, "F_shared (%d) %% 32 != 0 (blocks of 32 values share a scale)", s->F_shared);
+    // the scales of a workgroup's weight rows lie in LDS
+    if (s->d > 16384 || s->F > 32768 || s->F_shared > 32768)
+      return fail(MOE_ERR_UNSUPPORTED, "d (%d) > 16384, or F (%d) or F_shared (%d) > 32768, with 4-bit weights", s->d, s->F,
+                  s->F_shared);
   }
   if (s->T == 0) return ok();
   CHECK(check_ptr(x, 16, "x"));
@@ -228,6 +235,14 @@ int moe_layer_decode(const moe_shape_t* shape, const void* x, const void* w_rout
   if (shared) {
     CHECK(check_ptr(ws13, 16, "ws13"));
     CHECK(check_ptr(ws2, 16, "ws2"));
+  }
+  if (mx) {
+    CHECK(check_ptr(w13_scales, 16, "w13_scales"));
+    CHECK(check_ptr(w2_scales, 16, "w2_scales"));
+    if (shared) {
+      CHECK(check_ptr(ws13_scales, 16, "ws13_scales"));
+      CHECK(check_ptr(ws2_scales, 16, "ws2_scales"));
+    }
   }
   CHECK(check_ptr(out, 16, "out"));
   const DecodeLayout L = decode_layout(s);
@@ -262,6 +277,7 @@ int moe_layer_decode(const moe_shape_t* shape, const void* x, const void* w_rout
   p.ws2_scales = static_cast<const uint8_t*>(ws2_scales);
   p.act = at<moe::bf16_t>(ws, L.act);
   p.act_shared = at<moe::bf16_t>(ws, L.act_shared);
+  p.y = at<float>(ws, L.y);
   p.out = static_cast<moe::bf16_t*>(out);
   p.T = (int32_t)s->T;
   p.d = s->d;

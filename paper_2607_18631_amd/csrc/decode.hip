@@ -11,10 +11,19 @@
 //   gate     one wave per token (gate_device.hpp)
 //   plan     the experts that have rows and their slots: per expert the 64-bit mask of its tokens, so a
 //            slot's rank is a popcount and the order does not depend on the order of the writes
-//   up       16 features (gate and up rows) of one expert per workgroup, K dealt to its waves
-//   down     16 output columns per workgroup: units of (expert, K chunk) dealt to its waves, each wave
-//            adding its gate-weighted rows into token sums of its own in LDS; the waves' sums are added
-//            in order and rounded once.  The combine needs no launch and no atomics.
+//   up       a workgroup owns one expert and 16, 32 or 64 features of it (gate and up rows); its waves take
+//            16 features each, or parts of K of the same ones
+//   down     the same on the other weights; float32 rows for each slot
+//   combine  the token's rows times their gates, in slot order, and the shared expert's; rounded once
+//
+// What bounds it is the rate at which the weights arrive, so a wave keeps three units of them on their way and asks
+// the memory for nothing else: the token rows of its expert and the scales of its weights are staged in LDS first,
+// in whole lines.  (Fetched lane by lane next to the weights, they took more of the L1's accesses than the weights
+// did.)  Every load that the compiler sees in the loop is unconditional: behind one that may not have been issued, it
+// has to wait for all of them.
+#include <algorithm>
+#include <cmath>
+
 #include "common.hpp"
 #include "gate_device.hpp"
 #include "gemm_device.hpp"
@@ -24,9 +33,16 @@
 namespace moe {
 namespace {
 
-constexpr int kUnit = 256;        // K values of a unit: 8 operand fragments of 32
-constexpr int kUpWaves = 4;
-constexpr int kDownWaves = 8;
+// an offset past every buffer (they end below it)
+constexpr uint32_t kPast = 0x80000000u;
+
+// K values of a unit: the operand fragments of 32 values whose loads a wave issues together.  Two units of
+// weights are in its registers, one being multiplied and one on its way.
+template <bool MX>
+struct Unit {
+  static constexpr int FRAGS = MX ? 8 : 4;
+  static constexpr int K = 32 * FRAGS;
+};
 
 // Lane (r = l % 16, q = l / 16) holds 8 values of row r in fragment f of a unit; which 8 is free as long
 // as both operands agree.  bf16: every load takes 16 of the 128 bytes that the four q's lanes read of a
@@ -36,55 +52,41 @@ __device__ __forceinline__ int frag_k(int f, int q) {
   return MX ? 128 * (f / 4) + 32 * q + 8 * (f % 4) : 64 * (f / 2) + 16 * q + 8 * (f % 2);
 }
 
-// a row of weights, as this lane reads it (nullptr elements: a row that does not exist, zeros)
-struct WeightRow {
-  const char* elements;
-  const uint8_t* scales;
-};
-template <bool MX>
-__device__ __forceinline__ WeightRow weight_row(const void* w, const uint8_t* scales, int64_t row, int K, bool valid) {
-  WeightRow r;
-  r.elements = valid ? static_cast<const char*>(w) + row * (MX ? K / 2 : 2 * (int64_t)K) : nullptr;
-  r.scales = MX && valid ? scales + row * (K / 32) : nullptr;
-  return r;
+// Buffer of `bytes` bytes from a wave-uniform address: loads take a 32-bit offset per lane and give zeros
+// past the end, so rows and values that do not exist need no address of their own.  The check subtracts a load's
+// uniform offset from the buffer's size, so that offset has to lie inside the buffer.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer(const void* base, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)min(bytes, (int64_t)kPast), 0x00027000);
+}
+__device__ __forceinline__ u32x4 load16(Buffer b, uint32_t lane_offset, int uniform_offset) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, (int)lane_offset, uniform_offset, 0));
 }
 
-__device__ __forceinline__ u32x4 ld16_or_zero(const char* p, bool valid) {
-  return ld16(valid ? p : reinterpret_cast<const char*>(g_zero_chunk));
-}
-
-template <bool MX>
+// WHOLE: K is a multiple of the unit, so no load has to ask whether its values exist.
+template <bool MX, bool WHOLE>
 struct WeightUnit {
-  u32x4 v[MX ? 2 : 8];
-  uint32_t s[MX ? 2 : 1];
+  u32x4 v[MX ? 2 : 4];
 
-  __device__ __forceinline__ void load(const WeightRow& row, int k0, int K, int q) {
-    const bool on = row.elements != nullptr;
-    if constexpr (MX) {
+  // this lane's part of the unit at k0 of 16 rows of K values; not `on`: nothing is read
+  __device__ __forceinline__ void load(Buffer w, int r, int q, int k0, int K, bool on = true) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int b = k0 / 32 + 4 * i + q;
-        const bool in = on && b < K / 32;
-        v[i] = ld16_or_zero(row.elements + (int64_t)b * 16, in);
-        s[i] = *(in ? row.scales + b : reinterpret_cast<const uint8_t*>(g_zero_chunk));
-      }
-    } else {
-#pragma unroll
-      for (int f = 0; f < 8; ++f) {
-        const int k = k0 + frag_k<false>(f, q);
-        v[f] = ld16_or_zero(row.elements + (int64_t)k * 2, on && k < K);
-      }
+    for (int i = 0; i < (MX ? 2 : 4); ++i) {
+      const int k = frag_k<MX>(MX ? 4 * i : i, q);
+      v[i] = load16(w, on && (WHOLE || k0 + k < K) ? (MX ? (r * K + k) / 2 : 2 * (r * K + k)) : kPast,
+                                  MX ? k0 / 2 : 2 * k0);
     }
   }
-  __device__ __forceinline__ bf16x8 frag(int f) const {
+  // fragment f; scale: of this lane's block f / 4, as a float (4-bit weights).  The conversion looks at the scale's
+  // exponent bits alone: a zero field is 2^-127, 255 NaN.
+  __device__ __forceinline__ bf16x8 frag(int f, const float* scale) const {
     if constexpr (MX) {
       const uint32_t w = v[f / 4][f % 4];
-      const float scale = mx_scale(s[f / 4]);
       u32x4 r;
-      r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
-      r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
-      r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
-      r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+      r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale[f / 4], 0));
+      r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale[f / 4], 1));
+      r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale[f / 4], 2));
+      r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale[f / 4], 3));
       return __builtin_bit_cast(bf16x8, r);
     } else {
       return __builtin_bit_cast(bf16x8, v[f]);
@@ -92,61 +94,89 @@ struct WeightUnit {
   }
 };
 
-template <bool MX>
-__device__ __forceinline__ void load_rows(u32x4 (&b)[8], const bf16_t* row, int k0, int K, int q) {
+// FRAGS fragments of one lane's token row, which starts `row` bytes into the buffer (kPast: no token, zeros)
+template <bool MX, int FRAGS>
+struct RowUnit {
+  u32x4 v[FRAGS];
+  // fragments first .. first + FRAGS - 1 of the unit at k0
+  __device__ __forceinline__ void load(Buffer rows, uint32_t row, int q, int k0, int K, int first = 0) {
 #pragma unroll
-  for (int f = 0; f < 8; ++f) {
-    const int k = k0 + frag_k<MX>(f, q);
-    b[f] = ld16_or_zero(reinterpret_cast<const char*>(row) + (int64_t)k * 2, row != nullptr && k < K);
+    for (int f = 0; f < FRAGS; ++f) {
+      const int k = frag_k<MX>(first + f, q);
+      v[f] = load16(rows, k0 + k < K && row != kPast ? row + 2 * k : kPast, 2 * k0);
+    }
   }
-}
+};
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
 // ---------------- logits ----------------
-__global__ __launch_bounds__(256) void k_decode_logits(DecodeProblem p, int splits, int chunk) {
+// A workgroup: 16 experts, 16 tokens, one partial's share of K, a quarter of it per wave.
+__global__ __launch_bounds__(256) void k_decode_logits(DecodeProblem p, int chunk) {
+  __shared__ f32x4 s_sum[3][64];
   const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
-  const int e0 = blockIdx.x * 16, split = blockIdx.y * 4 + (threadIdx.x >> 6);
-  if (split >= splits) return;
-  const int k_end = min(p.d, (split + 1) * chunk);
-  const WeightRow w = weight_row<false>(p.w_router, nullptr, e0 + r, p.d, e0 + r < p.E);
-  f32x4 acc[4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int e0 = blockIdx.x * 16, t = blockIdx.y * 16 + r, split = blockIdx.z;
+  // the next kernel counts its workgroups here
+  if (blockIdx.x + blockIdx.y + blockIdx.z == 0 && threadIdx.x == 0) p.plan->arrived = 0;
+  const int begin = (split * 4 + wave) * chunk, end = min(p.d, begin + chunk);
+  const Buffer w = buffer(p.w_router + (int64_t)e0 * p.d, (int64_t)min(16, p.E - e0) * p.d * 2);
+  const Buffer x = buffer(p.x, (int64_t)p.T * p.d * 2);
+  const uint32_t row = t < p.T ? (uint32_t)t * p.d * 2 : kPast;
+  constexpr int UK = Unit<false>::K, IN_FLIGHT = 2;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int k0 = begin; k0 < end; k0 += IN_FLIGHT * UK) {
+    WeightUnit<false, false> u[IN_FLIGHT];
+    RowUnit<false, Unit<false>::FRAGS> b[IN_FLIGHT];
 #pragma unroll
-  for (int c = 0; c < 4; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int k0 = split * chunk; k0 < k_end; k0 += kUnit) {
-    WeightUnit<false> u;
-    u.load(w, k0, k_end, q);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      if (c * 16 < p.T) {
-        const int t = c * 16 + r;
-        u32x4 b[8];
-        load_rows<false>(b, t < p.T ? p.x + (int64_t)t * p.d : nullptr, k0, k_end, q);
-#pragma unroll
-        for (int f = 0; f < 8; ++f) acc[c] = mfma16(u.frag(f), b[f], acc[c]);
-      }
+    for (int i = 0; i < IN_FLIGHT; ++i) {
+      const int k = min(k0 + i * UK, p.d - 1) / 8 * 8;             // inside the row, past `end` or not
+      const int stop = k0 + i * UK < end ? end : 0;
+      u[i].load(w, r, q, k, p.d);                             // (weights past `end` meet zeros)
+      b[i].load(x, row, q, k, stop);
     }
+#pragma unroll
+    for (int i = 0; i < IN_FLIGHT; ++i)
+#pragma unroll
+      for (int f = 0; f < Unit<false>::FRAGS; ++f) acc = mfma16(u[i].frag(f, nullptr), b[i].v[f], acc);
   }
+  if (wave > 0) s_sum[wave - 1][lane] = acc;
+  __syncthreads();
+  if (wave == 0 && t < p.T) {
+    acc += s_sum[0][lane];
+    acc += s_sum[1][lane];
+    acc += s_sum[2][lane];
+    float* out = p.logits + ((int64_t)split * p.T + t) * p.E + e0 + 4 * q;
 #pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const int t = c * 16 + r;
-    if (t < p.T) {
-      float* out = p.logits + ((int64_t)split * p.T + t) * p.E + e0 + 4 * q;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (e0 + 4 * q + i < p.E) out[i] = acc[c][i];
-    }
+    for (int i = 0; i < 4; ++i)
+      if (e0 + 4 * q + i < p.E) out[i] = acc[i];
   }
 }
 
-// ---------------- plan ----------------
-__global__ __launch_bounds__(256) void k_decode_plan(DecodeProblem p) {
+// ---------------- gate and plan ----------------
+// One wave per token; the workgroup that ends last makes the plan from all tokens' choices.
+template <int PL>
+__global__ __launch_bounds__(256) void k_decode_gate(DecodeProblem p) {
+  __shared__ float s_key[4][64 * PL];
+  __shared__ float s_gscore[4][64];
   __shared__ unsigned long long s_mask[kMaxGroups];
-  __shared__ int s_begin[kMaxGroups];
-  __shared__ int s_tmp[4];
-  const int tid = threadIdx.x, n = p.T * p.top_k;
+  __shared__ int s_begin[kMaxGroups], s_tmp[4], s_last;
+  __shared__ uint32_t s_kept[kDecodeTokens];
+  const int tid = threadIdx.x, n = p.T * p.top_k, wave = tid >> 6;
+  const int64_t t = (int64_t)blockIdx.x * 4 + wave;
+  if (t < p.T) gate_token<PL>(p.gate, t, s_key[wave], s_gscore[wave]);
+  if (gridDim.x > 1) {
+    // the choices reach the device's memory before the count does, and are read back behind it
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) s_last = atomicAdd(&p.plan->arrived, 1) == (int)gridDim.x - 1;
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+  }
+  if (tid < kDecodeTokens) s_kept[tid] = 0;
   for (int e = tid; e < p.E_local; e += 256) s_mask[e] = 0ull;
   __syncthreads();
   for (int i = tid; i < n; i += 256) {
@@ -155,13 +185,13 @@ __global__ __launch_bounds__(256) void k_decode_plan(DecodeProblem p) {
   }
   __syncthreads();
   const int cap = p.expert_capacity > 0 ? p.expert_capacity : kDecodeTokens;
-  // four neighbouring experts per thread: rows in the low half, experts with rows in the high half
+  // four neighbouring experts per thread: rows in the low half, blocks of 16 of them in the high half
   int cnt[4], sum = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int e = 4 * tid + i;
     cnt[i] = e < p.E_local ? min(__popcll(s_mask[e]), cap) : 0;
-    sum += cnt[i] + (cnt[i] > 0 ? 1 << 16 : 0);
+    sum += cnt[i] + ((cnt[i] + 15) / 16 << 16);
   }
   int excl;
   const int total = block_exclusive_scan<256>(sum, s_tmp, excl);
@@ -169,199 +199,364 @@ __global__ __launch_bounds__(256) void k_decode_plan(DecodeProblem p) {
   for (int i = 0; i < 4; ++i) {
     if (cnt[i] > 0) {
       const int e = 4 * tid + i, a = excl >> 16, b = excl & 0xffff;
-      s_begin[e] = b;
-      p.plan->expert[a] = e;
-      p.plan->begin[a] = b;
-      excl += cnt[i] + (1 << 16);
+      s_begin[e] = b | a << 16;
+      for (int k = 0; 16 * k < cnt[i]; ++k) {
+        p.plan->entry[a + k].expert = e;
+        p.plan->entry[a + k].begin = b + 16 * k;
+        p.plan->entry[a + k].count = min(16, cnt[i] - 16 * k);
+      }
+      excl += cnt[i] + ((cnt[i] + 15) / 16 << 16);
     }
   }
-  if (tid == 0) {
-    p.plan->n_active = total >> 16;
-    p.plan->begin[total >> 16] = total & 0xffff;
-  }
+  const int most = decode_entries(p.T, p.top_k, p.E_local);
+  for (int a = (total >> 16) + tid; a < most; a += 256) p.plan->entry[a].count = 0;
   __syncthreads();
   for (int i = tid; i < n; i += 256) {
     const int e = p.gate.topk_idx[i] - p.e_begin;
     if (e >= 0 && e < p.E_local) {
       const int rank = __popcll(s_mask[e] & ((1ull << (i / p.top_k)) - 1));
-      if (rank < cap) p.plan->slot[s_begin[e] + rank] = i;
-    }
-  }
-}
-
-// ---------------- up ----------------
-// act[row_of(c)][f0 .. f0 + 15] = bf16(silu(gate) * up) for the m rows x[token_of(c)], c < m
-template <bool MX, int CB>
-__device__ __forceinline__ void up_tile(const DecodeProblem& p, const void* w13, const uint8_t* scales, int64_t wrow0,
-                                        int F, int f0, int m, const int32_t* slots, bf16_t* act, float* s_red) {
-  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
-  const int K = p.d, units = (K + kUnit - 1) / kUnit;
-  const bool in = f0 + r < F;
-  const WeightRow gate = weight_row<MX>(w13, scales, wrow0 + f0 + r, K, in);
-  const WeightRow up = weight_row<MX>(w13, scales, wrow0 + F + f0 + r, K, in);
-  const bf16_t* x[CB];
-#pragma unroll
-  for (int c = 0; c < CB; ++c) {
-    const int i = c * 16 + r;
-    x[c] = nullptr;
-    if (i < m) x[c] = p.x + (int64_t)(slots ? slots[i] / p.top_k : i) * K;
-  }
-  f32x4 acc[2][CB];
-#pragma unroll
-  for (int c = 0; c < CB; ++c) acc[0][c] = acc[1][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int u = wave; u < units; u += kUpWaves) {
-    WeightUnit<MX> wg, wu;
-    wg.load(gate, u * kUnit, K, q);
-    wu.load(up, u * kUnit, K, q);
-#pragma unroll
-    for (int c = 0; c < CB; ++c) {
-      u32x4 b[8];
-      load_rows<MX>(b, x[c], u * kUnit, K, q);
-#pragma unroll
-      for (int f = 0; f < 8; ++f) {
-        acc[0][c] = mfma16(wg.frag(f), b[f], acc[0][c]);
-        acc[1][c] = mfma16(wu.frag(f), b[f], acc[1][c]);
+      if (rank < cap) {
+        p.plan->slot[(s_begin[e] & 0xffff) + rank] = i;
+        if (rank % 16 == 0) p.plan->entry[(s_begin[e] >> 16) + rank / 16].first = i;
+        atomicOr(&s_kept[i / p.top_k], 1u << (i % p.top_k));
       }
     }
   }
-  // the waves' sums, added in wave order
-  f32x4* red = reinterpret_cast<f32x4*>(s_red);
-#pragma unroll
-  for (int c = 0; c < CB; ++c) {
-    red[((wave * 2 + 0) * CB + c) * 64 + lane] = acc[0][c];
-    red[((wave * 2 + 1) * CB + c) * 64 + lane] = acc[1][c];
-  }
   __syncthreads();
-  for (int c = wave; c < CB; c += kUpWaves) {
-    f32x4 h = red[c * 64 + lane], u = red[(CB + c) * 64 + lane];
-#pragma unroll
-    for (int w = 1; w < kUpWaves; ++w) {
-      h += red[((w * 2 + 0) * CB + c) * 64 + lane];
-      u += red[((w * 2 + 1) * CB + c) * 64 + lane];
-    }
-    const int i = c * 16 + r;
-    if (i < m && f0 + 4 * q < F) {
-      float a[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) a[j] = h[j] / (1.0f + expf(-h[j])) * u[j];
-      const u32x2 v = {pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])};
-      *reinterpret_cast<u32x2*>(act + (int64_t)(slots ? slots[i] : i) * F + f0 + 4 * q) = v;
-    }
-  }
+  if (tid < p.T) p.plan->kept[tid] = s_kept[tid];
 }
 
+// ---------------- the experts' products ----------------
+constexpr int kWaves = 4;
+// units of weights a wave has on their way
 template <bool MX>
-__global__ __launch_bounds__(64 * kUpWaves, 4) void k_decode_up(DecodeProblem p, int shared_tiles, int tiles) {
-  __shared__ __align__(16) float s_red[kUpWaves * 2 * 4 * 64 * 4];
-  const void* w13 = p.ws13;
-  const uint8_t* scales = p.ws13_scales;
-  int64_t wrow0 = 0;
-  int F = p.F_shared, m = p.T, tile = blockIdx.x;
-  const int32_t* slots = nullptr;
+constexpr int kStages = MX ? 4 : 3;
+
+// One launch's geometry: `split` waves share the same 16 features (each takes every split-th unit of K), so a
+// workgroup owns 16 * kWaves / split features; `room` bytes of LDS hold rows.
+struct Geometry {
+  int32_t tiles, shared_tiles;     // workgroups per entry of the plan, per 16 tokens of the shared expert
+  int32_t shared;                  // workgroups of the shared expert
+  int32_t split, shared_split, room;
+};
+__host__ __device__ constexpr int features_of(int split) { return 16 * kWaves / split; }
+// bytes between rows of K values in LDS: 16 past the row, so that the four rows and four q's that a read touches at
+// once lie in different banks
+__host__ __device__ constexpr int row_bytes(int K) { return 2 * K + 16; }
+
+// What a workgroup multiplies: m rows of `rows` (row_at(i) bytes into it) by weight rows [row0, ..) of K values,
+// NS streams (gate and up) of them `stream` rows apart.
+struct Product {
+  const void* w;
+  const uint8_t* scales;
+  const bf16_t* rows;
+  int64_t row0;
+  int32_t stream, K, features, f0, m;
+  const int32_t* slots;            // of the rows; nullptr: row i is token first + i
+  int32_t first;                   // slots[0]
+  int32_t per_token;               // slots per row of `rows`: top_k (token rows), or 1 (rows of slots)
+  // slot of this lane's row r (a lane without one: the last row's)
+  __device__ __forceinline__ int slot_of_lane(int r) const {
+    const int i = min(r, m - 1);
+    int s = first + (slots ? 0 : i);
+    if (slots && m > 1) s = slots[i];
+    return s;
+  }
+};
+
+// acc[s]: features f0w + 4 q + j of row r, for this wave's part of K (of `split` parts)
+template <bool MX, bool WHOLE, int NS>
+__device__ __forceinline__ void multiply(const Product& p, int slot, int f0w, int part, int split, int room, char* lds,
+                                         f32x4 (&acc)[NS]) {
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int UK = Unit<MX>::K, FRAGS = Unit<MX>::FRAGS, STAGES = kStages<MX>;
+  const int K = p.K, units = (K + UK - 1) / UK, KB = K / 32;
+  // rows that exist; a wave past them all computes the last one again (its results are not used)
+  const int n = max(1, min(16, p.features - f0w));
+  const int64_t wbytes = MX ? K / 2 : 2 * (int64_t)K;
+  Buffer w[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const int64_t row = p.row0 + (int64_t)s * p.stream + min(f0w, p.features - 1);
+    w[s] = buffer(static_cast<const char*>(p.w) + row * wbytes, n * wbytes);
+    acc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  struct Stage {
+    WeightUnit<MX, WHOLE> w[NS];
+  };
+  const int count = part < units ? (units - part + split - 1) / split : 0;   // this wave's units
+  const int rounds = (units + split - 1) / split;                            // the most any wave has
+  // the wave's unit i; past the last, loads all the same (they stay unconditional) but of nothing
+  auto load = [&](Stage& st, int i) {
+    const int u = min(part + split * i, units - 1);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) st.w[s].load(w[s], r, q, u * UK, K, i < count);
+  };
+
+  // ---- LDS: the scales of all the workgroup's weight rows, then its token rows, as many rounds of K at a time as
+  // there is room for; copied straight from memory ----
+  auto copy = [&](const char* src, char* dst, int vectors) {       // of 16 bytes; waves take 64 in turn
+    for (int c = 64 * wave; c < vectors; c += 64 * kWaves)
+      if (c + lane < vectors) dma16_v(src + 16 * (int64_t)(c + lane), reinterpret_cast<bf16_t*>(dst + 16 * c));
+  };
+  const int tile = features_of(split);
+  char* s_rows = lds + (MX ? NS * tile * KB : 0);
+  const int per_round = split * UK;                                // values of K
+  const int row = p.per_token > 1 ? slot / p.per_token : slot;
+  const int held = max(1, min(rounds, (room / p.m - 16) / (2 * per_round)));   // rounds in LDS
+  const int pitch = row_bytes(min(held * per_round, K));
+  auto copy_rows = [&](int round) {
+    const int k0 = round * per_round, len = min(held * per_round, K - k0);
+    for (int i = 0; i < p.m; ++i)                                  // (no load in here: see above)
+      copy(reinterpret_cast<const char*>(p.rows) + 2 * ((int64_t)__builtin_amdgcn_readlane(row, i) * K + k0),
+           s_rows + i * pitch, len / 8);
+  };
+  copy_rows(0);
+  if constexpr (MX) {
+    // 16 rows' scales are K / 2 bytes, whole vectors of 16; features come in 32s
+    const int bytes = min(tile, p.features - p.f0) * KB;
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      copy(reinterpret_cast<const char*>(p.scales) + (p.row0 + (int64_t)s * p.stream + p.f0) * KB, lds + s * tile * KB,
+           bytes / 16);
+  }
+  Stage st[STAGES];
+#pragma unroll
+  for (int i = 0; i < STAGES; ++i) load(st[i], i);
+  // the copies have landed, and the first unit's loads, when at most the other units' are on their way
+  wait_vmcnt<(STAGES - 1) * NS * (MX ? 2 : 4)>();
+  raw_barrier();
+
+  const uint8_t* my_scales = reinterpret_cast<const uint8_t*>(lds) + (f0w - p.f0 + r) * KB;
+  const char* mine = s_rows + min(r, p.m - 1) * pitch;             // a column without a row reads the last row
+  auto step = [&](Stage& now, int i, int first) {                  // round i, rounds from `first` in LDS
+    const int k0 = (part + split * i) * UK, base = first * per_round;
+    float scale[NS][2];
+    if constexpr (MX) {
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int b = k0 / 32 + 4 * j + q;
+          scale[s][j] = __uint_as_float((uint32_t)my_scales[s * tile * KB + (WHOLE ? b : min(b, KB - 1))] << 23);
+        }
+    }
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f) {
+      const int k = k0 + frag_k<MX>(f, q);
+      u32x4 b = ld16(mine + 2 * ((WHOLE ? k : min(k, K - 8)) - base));
+      if (!WHOLE && k >= K) b = u32x4{0, 0, 0, 0};                 // values that do not exist: zeros times zeros
+#pragma unroll
+      for (int s = 0; s < NS; ++s) acc[s] = mfma16(now.w[s].frag(f, scale[s]), b, acc[s]);
+    }
+  };
+  int first = 0;
+  for (int i = 0; i < rounds; i += STAGES) {
+#pragma unroll
+    for (int j = 0; j < STAGES; ++j) {
+      if (i + j == first + held && i + j < rounds) {               // the same for every wave
+        lds_barrier();                                             // everybody has read the rounds held
+        first = i + j;
+        copy_rows(first);
+        wait_vmcnt<0>();
+        raw_barrier();
+      }
+      if (i + j < count) step(st[j], i + j, first);
+      load(st[j], i + j + STAGES);
+    }
+  }
+  __syncthreads();                                                 // the LDS is used again
+}
+
+// Multiplies, adds the parts of K in order, and hands each lane of the waves with part 0 its results:
+// done(slot, f, sums) for its row's slot and features f .. f + 3.
+template <bool MX, bool WHOLE, int NS, class Done>
+__device__ __forceinline__ void product(const Product& p, int split, int room, char* lds, Done&& done) {
+  const int lane = threadIdx.x & 63, r = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % split;
+  const int f0w = p.f0 + 16 * (wave / split);
+  f32x4 acc[NS];
+  const int slot = p.slot_of_lane(r);
+  multiply<MX, WHOLE, NS>(p, slot, f0w, part, split, room, lds, acc);
+  if (split > 1) {
+    f32x4* red = reinterpret_cast<f32x4*>(lds);
+    if (part > 0)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) red[(wave * NS + s) * 64 + lane] = acc[s];
+    __syncthreads();
+    if (part == 0)
+      for (int w = wave + 1; w < wave + split; ++w)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) acc[s] += red[(w * NS + s) * 64 + lane];
+  }
+  if (part == 0 && r < p.m && f0w + 4 * q < p.features) done(slot, f0w + 4 * q, acc);
+}
+constexpr int kRedBytes = kWaves * 2 * 64 * 16;        // the parts' sums at most
+
+// The shared expert's workgroups come first (16 tokens and some features each), then those of the plan's entries.
+template <bool MX, bool WHOLE>
+__global__ __launch_bounds__(64 * kWaves, MX ? 4 : 3) void k_decode_up(DecodeProblem p, Geometry g) {
+  extern __shared__ __align__(16) char lds[];
+  const int b = (int)blockIdx.x - g.shared, first = blockIdx.x / g.shared_tiles * 16;
+  Product o{p.ws13, p.ws13_scales, p.x, 0, p.F_shared, p.d, p.F_shared,
+            (int)(blockIdx.x % g.shared_tiles) * features_of(g.shared_split), min(16, p.T - first), nullptr, first, 1};
   bf16_t* act = p.act_shared;
-  if (tile >= shared_tiles) {
-    const int a = (tile - shared_tiles) / tiles;
-    if (a >= p.plan->n_active) return;
-    tile = (tile - shared_tiles) % tiles;
-    const int b = p.plan->begin[a];
-    w13 = p.w13;
-    scales = p.w13_scales;
-    F = p.F;
-    wrow0 = (int64_t)p.plan->expert[a] * 2 * F;
-    m = p.plan->begin[a + 1] - b;
-    slots = p.plan->slot + b;
+  int split = g.shared_split;
+  if (b >= 0) {
+    const DecodePlan::Entry e = p.plan->entry[b / g.tiles];
+    if (e.count == 0) return;
+    split = g.split;
+    o.w = p.w13;
+    o.scales = p.w13_scales;
+    o.features = o.stream = p.F;
+    o.row0 = (int64_t)e.expert * 2 * p.F;
+    o.f0 = b % g.tiles * features_of(split);
+    o.m = e.count;
+    o.slots = p.plan->slot + e.begin;
+    o.first = e.first;
+    o.per_token = p.top_k;
     act = p.act;
   }
-  if (m <= 16) up_tile<MX, 1>(p, w13, scales, wrow0, F, tile * 16, m, slots, act, s_red);
-  else if (m <= 32) up_tile<MX, 2>(p, w13, scales, wrow0, F, tile * 16, m, slots, act, s_red);
-  else up_tile<MX, 4>(p, w13, scales, wrow0, F, tile * 16, m, slots, act, s_red);
+  product<MX, WHOLE, 2>(o, split, g.room, lds, [&](int slot, int f, const f32x4 (&s)[2]) {
+    float v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = s[0][j] / (1.0f + expf(-s[0][j])) * s[1][j];
+    const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    *reinterpret_cast<u32x2*>(act + (int64_t)slot * o.features + f) = w;
+  });
 }
 
-// ---------------- down and combine ----------------
-template <bool MX>
-__global__ __launch_bounds__(64 * kDownWaves, 2) void k_decode_down(DecodeProblem p) {
-  // every wave's sums of the tokens' 16 columns
-  extern __shared__ __align__(16) float s_sum[];
-  __shared__ int s_begin[kDecodeSlots + 1], s_expert[kDecodeSlots], s_slot[kDecodeSlots];
-  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, q = lane >> 4, wave = tid >> 6;
-  const int T = p.T, d0 = blockIdx.x * 16;
-  const int n_active = p.plan->n_active;
-  for (int i = tid; i <= n_active; i += 64 * kDownWaves) {
-    s_begin[i] = p.plan->begin[i];
-    if (i < n_active) s_expert[i] = p.plan->expert[i];
+template <bool MX, bool WHOLE>
+__global__ __launch_bounds__(64 * kWaves, 4) void k_decode_down(DecodeProblem p, Geometry g) {
+  extern __shared__ __align__(16) char lds[];
+  const int b = (int)blockIdx.x - g.shared, first = blockIdx.x / g.shared_tiles * 16;
+  Product o{p.ws2, p.ws2_scales, p.act_shared, 0, 0, p.F_shared, p.d,
+            (int)(blockIdx.x % g.shared_tiles) * features_of(g.shared_split), min(16, p.T - first), nullptr, first, 1};
+  float* y = p.y + (int64_t)p.T * p.top_k * p.d;
+  int split = g.shared_split;
+  if (b >= 0) {
+    const DecodePlan::Entry e = p.plan->entry[b / g.tiles];
+    if (e.count == 0) return;
+    split = g.split;
+    o.w = p.w2;
+    o.scales = p.w2_scales;
+    o.rows = p.act;
+    o.row0 = (int64_t)e.expert * p.d;
+    o.K = p.F;
+    o.f0 = b % g.tiles * features_of(split);
+    o.m = e.count;
+    o.slots = p.plan->slot + e.begin;
+    o.first = e.first;
+    y = p.y;
   }
-  const int rows = p.plan->begin[n_active];
-  for (int i = tid; i < rows; i += 64 * kDownWaves) s_slot[i] = p.plan->slot[i];
-  for (int i = tid; i < kDownWaves * T * 16; i += 64 * kDownWaves) s_sum[i] = 0.f;
-  __syncthreads();
-  float* mine = s_sum + (int64_t)wave * T * 16;
-  const int per = (p.F + kUnit - 1) / kUnit, per_s = (p.F_shared + kUnit - 1) / kUnit;
-  const int routed = n_active * per, units = routed + per_s;
-  for (int u = wave; u < units; u += kDownWaves) {
-    const bool shared = u >= routed;
-    const int a = shared ? 0 : u / per, k0 = (shared ? u - routed : u % per) * kUnit;
-    const int F = shared ? p.F_shared : p.F, begin = shared ? 0 : s_begin[a];
-    const int m = shared ? T : s_begin[a + 1] - begin;
-    const int64_t wrow = (shared ? 0 : (int64_t)s_expert[a] * p.d) + d0 + r;
-    const WeightRow row = weight_row<MX>(shared ? p.ws2 : p.w2, shared ? p.ws2_scales : p.w2_scales, wrow, F, d0 + r < p.d);
-    WeightUnit<MX> w;
-    w.load(row, k0, F, q);
-    for (int c = 0; c < m; c += 16) {
-      const bool on = c + r < m;
-      int t = c + r;
-      float g = 1.0f;
-      const bf16_t* act = nullptr;
-      if (on && shared) act = p.act_shared + (int64_t)t * F;
-      if (on && !shared) {
-        const int slot = s_slot[begin + c + r];
-        t = slot / p.top_k;
-        g = p.gate.topk_w[slot];
-        act = p.act + (int64_t)slot * F;
-      }
-      u32x4 b[8];
-      load_rows<MX>(b, act, k0, F, q);
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int f = 0; f < 8; ++f) acc = mfma16(w.frag(f), b[f], acc);
-      if (on) {
-        f32x4* s = reinterpret_cast<f32x4*>(mine + t * 16 + 4 * q);
-        *s = *s + acc * g;
-      }
+  product<MX, WHOLE, 1>(o, split, g.room, lds, [&](int slot, int f, const f32x4 (&s)[1]) {
+    *reinterpret_cast<f32x4*>(y + (int64_t)slot * p.d + f) = s[0];
+  });
+}
+
+// ---------------- combine ----------------
+// out[t] = bf16(sum over the token's kept slots of gate * row, in slot order, + the shared expert's row); 4 columns
+// per thread
+__global__ __launch_bounds__(256) void k_decode_combine(DecodeProblem p) {
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 4, t = blockIdx.y;
+  if (c >= p.d) return;
+  const uint32_t kept = p.plan->kept[t];
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int j = 0; j < p.top_k; ++j)
+    if (kept >> j & 1) {
+      const int64_t slot = (int64_t)t * p.top_k + j;
+      s += *reinterpret_cast<const f32x4*>(p.y + slot * p.d + c) * p.gate.topk_w[slot];
     }
-  }
-  __syncthreads();
-  // 8 columns per thread
-  for (int i = tid; i < 2 * T; i += 64 * kDownWaves) {
-    const int t = i >> 1, c = 8 * (i & 1);
-    if (d0 + c < p.d) {
-      float v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = 0.f;
-      for (int w = 0; w < kDownWaves; ++w)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += s_sum[(w * T + t) * 16 + c + j];
-      st16(p.out + (int64_t)t * p.d + d0 + c, pack8(v));
-    }
-  }
+  if (p.F_shared) s += *reinterpret_cast<const f32x4*>(p.y + ((int64_t)p.T * p.top_k + t) * p.d + c);
+  *reinterpret_cast<u32x2*>(p.out + (int64_t)t * p.d + c) = u32x2{pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3])};
+}
+
+// ---------------- launches ----------------
+// experts that have rows when every token chooses at random (geometry only)
+double expected_active(const DecodeProblem& p) {
+  const double none = std::pow(1.0 - (double)p.top_k / p.E, p.T);
+  return std::max(1.0, p.E_local * (1.0 - none));
+}
+
+// `features` x K weights of each expert, ns streams of them (`features_s` x K_s of the shared expert)
+Geometry geometry(const DecodeProblem& p, int features, int K, int features_s, int K_s, int ns, bool mx, size_t& lds) {
+  Geometry g{};
+  auto tiles = [](int features, int split) { return (features + features_of(split) - 1) / features_of(split); };
+  // Waves on the same features: fewer where there are many workgroups (rows staged once serve more weights), more
+  // where there are few.  The shared expert's rows are all the tokens; its workgroups come first.
+  const double waves = expected_active(p) * ((features + 15) / 16);
+  g.split = waves >= 8192 ? 1 : waves >= 512 ? 2 : 4;
+  g.shared_split = 2;
+  g.tiles = tiles(features, g.split);
+  g.shared_tiles = std::max(1, tiles(features_s, g.shared_split));
+  g.shared = p.F_shared ? g.shared_tiles * ((p.T + 15) / 16) : 0;
+  // LDS: scales, and rows: room for all of an expert's rows where that leaves four workgroups per compute unit, else
+  // as much as leaves two.  A round of the most rows has to fit.
+  const int widest = std::max(K, p.F_shared ? K_s : 0), split = std::max(g.split, g.shared_split);
+  const int64_t fixed = mx ? (int64_t)ns * std::max(features_of(g.split), features_of(g.shared_split)) * (widest / 32) : 0;
+  const double rows = (double)p.T * p.top_k / p.E * p.E_local / expected_active(p);
+  const int most = std::min(p.T, 16);
+  const int64_t least = (int64_t)most * row_bytes(std::min(split * (mx ? Unit<true>::K : Unit<false>::K), widest));
+  const int64_t all = (int64_t)most * row_bytes((widest + split * 256 - 1) / (split * 256) * (split * 256));
+  const int64_t room = std::max(least, (rows > 1.25 ? 76 : 38) * 1024 - fixed);
+  g.room = (int)std::min(room, std::max(all, least));
+  lds = (size_t)std::max<int64_t>(kRedBytes, g.room + fixed);
+  return g;
+}
+
+constexpr size_t kMostLds = 158 * 1024;
+template <class Kernel>
+hipError_t launch_product(Kernel kernel, OccCache& cache, const DecodeProblem& p, const Geometry& g, size_t lds,
+                          hipStream_t stream) {
+  if (lds > kMostLds) return hipErrorInvalidValue;
+  // (the limit of 64 KiB of dynamic LDS is raised once per device and kernel)
+  hipError_t err = hipSuccess;
+  if (kernel_occupancy(cache, reinterpret_cast<const void*>(kernel), 64 * kWaves, kMostLds, err) <= 0) return err;
+  const int64_t blocks = g.shared + (int64_t)decode_entries(p.T, p.top_k, p.E_local) * g.tiles;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kWaves), lds, stream, p, g);
+  return hipGetLastError();
+}
+
+template <bool MX, bool WHOLE>
+hipError_t launch_up(const DecodeProblem& p, hipStream_t stream) {
+  static OccCache cache;
+  size_t lds;
+  const Geometry g = geometry(p, p.F, p.d, p.F_shared, p.d, 2, MX, lds);
+  return launch_product(k_decode_up<MX, WHOLE>, cache, p, g, lds, stream);
+}
+template <bool MX, bool WHOLE>
+hipError_t launch_down(const DecodeProblem& p, hipStream_t stream) {
+  static OccCache cache;
+  size_t lds;
+  const Geometry g = geometry(p, p.d, p.F, p.d, p.F_shared, 1, MX, lds);
+  return launch_product(k_decode_down<MX, WHOLE>, cache, p, g, lds, stream);
+}
+
+template <int PL>
+hipError_t launch_decode_gate(const DecodeProblem& p, hipStream_t stream) {
+  hipLaunchKernelGGL(k_decode_gate<PL>, dim3((p.T + 3) / 4), dim3(256), 0, stream, p);
+  return hipGetLastError();
 }
 
 template <bool MX>
 hipError_t launch_as(const DecodeProblem& p, hipStream_t stream) {
   const int splits = decode_logits_splits(p.E, p.d);
-  const int chunk = ((p.d + kUnit - 1) / kUnit + splits - 1) / splits * kUnit;
-  hipLaunchKernelGGL(k_decode_logits, dim3((p.E + 15) / 16, (splits + 3) / 4), dim3(256), 0, stream, p, splits, chunk);
+  const int chunk = ((p.d + 63) / 64 + 4 * splits - 1) / (4 * splits) * 64;
+  hipLaunchKernelGGL(k_decode_logits, dim3((p.E + 15) / 16, (p.T + 15) / 16, splits), dim3(256), 0, stream, p, chunk);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if ((e = launch_gate(p.gate, stream)) != hipSuccess) return e;
-  hipLaunchKernelGGL(k_decode_plan, dim3(1), dim3(256), 0, stream, p);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  const int tiles = (p.F + 15) / 16, shared_tiles = (p.F_shared + 15) / 16;
-  const int active = p.E_local < p.T * p.top_k ? p.E_local : p.T * p.top_k;
-  hipLaunchKernelGGL(k_decode_up<MX>, dim3(shared_tiles + active * tiles), dim3(64 * kUpWaves), 0, stream, p,
-                     shared_tiles, tiles);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(k_decode_down<MX>, dim3((p.d + 15) / 16), dim3(64 * kDownWaves),
-                     sizeof(float) * kDownWaves * p.T * 16, stream, p);
+  e = p.E <= 64 ? launch_decode_gate<1>(p, stream) : p.E <= 128 ? launch_decode_gate<2>(p, stream)
+      : p.E <= 256 ? launch_decode_gate<4>(p, stream) : p.E <= 512 ? launch_decode_gate<8>(p, stream)
+                                                                   : launch_decode_gate<16>(p, stream);
+  if (e != hipSuccess) return e;
+  constexpr int UK = Unit<MX>::K;
+  e = p.d % UK == 0 ? launch_up<MX, true>(p, stream) : launch_up<MX, false>(p, stream);
+  if (e != hipSuccess) return e;
+  e = p.F % UK == 0 && p.F_shared % UK == 0 ? launch_down<MX, true>(p, stream) : launch_down<MX, false>(p, stream);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_decode_combine, dim3((p.d + 1023) / 1024, p.T), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 

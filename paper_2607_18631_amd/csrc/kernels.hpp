@@ -6,6 +6,12 @@
 
 #include <mutex>
 
+#ifdef __HIPCC__
+#define MOE_HOST_DEVICE __host__ __device__
+#else
+#define MOE_HOST_DEVICE
+#endif
+
 namespace moe {
 
 typedef uint16_t bf16_t;
@@ -329,15 +335,24 @@ hipError_t launch_mx_gemm(const MxGemmProblem& p, hipStream_t stream);
 // Few-token layer: at most kDecodeTokens tokens, so the tokens of an expert are a 64-bit mask.
 constexpr int kDecodeTokens = 64;
 constexpr int kDecodeSlots = kDecodeTokens * 16;
-// The experts that have rows, written by the kernels: expert a of n_active owns the slots (token *
-// top_k + choice, ascending token) slot[begin[a]] .. slot[begin[a + 1] - 1].
+// The experts' rows in blocks of up to 16, written by the kernels: an entry (in expert order; count 0 past the last)
+// owns the slots (token * top_k + choice, ascending token) slot[begin] .. slot[begin + count - 1], the first of them
+// repeated.
 struct DecodePlan {
-  int32_t n_active;
-  int32_t expert[kDecodeSlots];
-  int32_t begin[kDecodeSlots + 1];
+  struct Entry {
+    int32_t expert, begin, count, first;
+  };
+  Entry entry[kDecodeSlots + kDecodeSlots / 16];
   int32_t slot[kDecodeSlots];
+  uint32_t kept[kDecodeTokens];    // bit j: the token's slot j is local and kept
+  int32_t arrived;                 // workgroups of the gate that are done
 };
-// K chunks of the router logits
+// entries of the plan at most: each expert with rows has one that is not full
+MOE_HOST_DEVICE inline int decode_entries(int T, int top_k, int E_local) {
+  const int slots = T * top_k;
+  return (E_local < slots ? E_local : slots) + (T > 16 ? slots / 16 : 0);
+}
+// partials of the router logits
 int decode_logits_splits(int E, int d);
 struct DecodeProblem {
   const bf16_t* x;            // [T, d]
@@ -349,6 +364,7 @@ struct DecodeProblem {
   const uint8_t *w13_scales, *w2_scales, *ws13_scales, *ws2_scales;
   bf16_t* act;                // [T * top_k, F], row = slot
   bf16_t* act_shared;         // [T, F_shared]
+  float* y;                   // [T * top_k + T, d], the slots' rows, then the shared expert's
   bf16_t* out;                // [T, d]
   int32_t T, d, E, top_k, e_begin, E_local, F, F_shared, expert_capacity;
 };

@@ -342,8 +342,7 @@ hipError_t launch_as(const MxGemmProblem& p, hipStream_t stream) {
 
 template <class T>
 hipError_t launch_tile(const MxGemmProblem& p, hipStream_t stream) {
-  // whole slices with scales that 4-byte copies can fetch, or slices with an end inside
-  const bool whole = p.K % kSlice == 0 && ((uintptr_t)p.X_scales | (uintptr_t)p.W_scales) % 4 == 0;
+  const bool whole = p.K % kSlice == 0;    // no slice has a row's end inside
   if (p.swiglu) return whole ? launch_as<T, true, true>(p, stream) : launch_as<T, true, false>(p, stream);
   return whole ? launch_as<T, false, true>(p, stream) : launch_as<T, false, false>(p, stream);
 }

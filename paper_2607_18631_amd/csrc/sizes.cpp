@@ -51,12 +51,12 @@ PermuteWs permute_ws(int64_t T, int E_local) {
   return w;
 }
 
-// Few-token layer: one wave multiplies 16 experts by a chunk of K for all tokens; chunks of at least
-// 256 values, at most 16 of them (the gate adds the partials).
+// Few-token layer: partials of the logits, which the gate adds.  A workgroup's four waves share one; a wave has 256
+// values of K at least.
 int decode_logits_splits(int E, int d) {
   (void)E;
-  const int s = (d + 255) / 256;
-  return s < 16 ? s : 16;
+  const int s = (d + 1023) / 1024;
+  return s < 4 ? s : 4;
 }
 
 // Norm backward: every workgroup leaves one row of partial sums of dgamma.  Four workgroups per

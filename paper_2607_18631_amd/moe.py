@@ -52,6 +52,8 @@ class MoEError(RuntimeError):
 
 _lib = None
 _vp = ctypes.c_void_p
+# torch's names that the calls below take, from lib() on (importing this module does not import torch)
+_bf16 = _f32 = _i32 = _u8 = _raw_stream = _current_device = None
 
 
 def lib():
@@ -64,7 +66,10 @@ def lib():
         # one the library is linked against.  Loading torch first makes the library bind to that
         # runtime; loaded the other way round, the process holds two runtimes and the library's
         # kernels are not found for torch's device memory ("invalid device function").
-        import torch  # noqa: F401
+        import torch
+        global _bf16, _f32, _i32, _u8, _raw_stream, _current_device
+        _bf16, _f32, _i32, _u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+        _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
         L = ctypes.CDLL(LIB_PATH)
         sp = ctypes.POINTER(MoEShapeC)
         L.moe_abi_version.restype = ctypes.c_int
@@ -215,34 +220,56 @@ def _refuse(message: str):
     raise MoEError(MOE_ERR_INVALID_ARG, message)
 
 
+def _mismatch(device, name, t, dtype, wanted):
+    _refuse(f"{name} is missing" if t is None else
+            f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; "
+            f"expected contiguous {dtype} {wanted} on {device}")
+
+
 def _take(device, name, t, dtype, *shape):
     """Pointer of a tensor that has to have this dtype and shape on this device."""
-    if t is None:
-        _refuse(f"{name} is missing")
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; "
-                f"expected contiguous {dtype} {shape} on {device}")
+    if t is None or t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        _mismatch(device, name, t, dtype, shape)
     return t.data_ptr()
+
+
+def _bytes(device, name, t, n):
+    """Pointer of a contiguous uint8 tensor of at least n values (any shape)."""
+    if t is None or t.dtype is not _u8 or t.numel() < n or t.device != device or not t.is_contiguous():
+        _mismatch(device, name, t, _u8, f"of {n} values")
+    return t.data_ptr()
+
+
+def _ws(device, ws):
+    """(pointer, bytes) of a workspace."""
+    return (None, 0) if ws is None else (_bytes(device, "ws", ws, 0), ws.numel())
+
+
+def _matrix(name, t):
+    """(rows, columns, device) of a tensor on a GPU."""
+    lib()
+    if t.dim() != 2:
+        _refuse(f"{name} has {t.dim()} dimensions, expected 2")
+    if not t.is_cuda:
+        _refuse(f"{name} is on {t.device}, not on a GPU")
+    rows, cols = t.shape
+    return rows, cols, t.device
 
 
 def _on(device, stream, call, *args):
     """Runs a library call on ``device`` and ``stream`` (None: that device's current stream)."""
-    import torch
-    if device.type != "cuda":
-        _refuse(f"tensors are on {device}, not on a GPU")
+    index = device.index
     if stream is None:
-        stream = torch.cuda.current_stream(device).cuda_stream
-    if device.index == torch.cuda.current_device():
-        _check(call(*args, stream))
+        # the handle of torch.cuda.current_stream(device), without a Stream object (1.7 us a call)
+        stream = _raw_stream(index)
+    if index == _current_device():
+        status = call(*args, stream)
     else:
-        with torch.cuda.device(device):
-            _check(call(*args, stream))
-
-
-def _matrix(name, t):
-    if t.dim() != 2:
-        _refuse(f"{name} has {t.dim()} dimensions, expected 2")
-    return t.shape
+        import torch
+        with torch.cuda.device(index):
+            status = call(*args, stream)
+    if status != MOE_OK:
+        raise MoEError(status, last_error())
 
 
 def mx_elements_per_row(format: int, cols: int) -> int:
@@ -252,77 +279,48 @@ def mx_elements_per_row(format: int, cols: int) -> int:
 
 def moe_mx_quantize(format, x, elements, scales, stream=None):
     """bf16 ``x [rows, cols]`` into uint8 ``elements [rows, cols / 2 or cols]`` and ``scales [rows, cols / 32]``."""
-    import torch
-    rows, cols = _matrix("x", x)
-    dev, u8 = x.device, torch.uint8
-    _on(dev, stream, lib().moe_mx_quantize, rows, cols, format, _take(dev, "x", x, torch.bfloat16, rows, cols),
-        _take(dev, "elements", elements, u8, rows, mx_elements_per_row(format, cols)),
-        _take(dev, "scales", scales, u8, rows, cols // 32))
+    rows, cols, dev = _matrix("x", x)
+    _on(dev, stream, _lib.moe_mx_quantize, rows, cols, format, _take(dev, "x", x, _bf16, rows, cols),
+        _take(dev, "elements", elements, _u8, rows, mx_elements_per_row(format, cols)),
+        _take(dev, "scales", scales, _u8, rows, cols // 32))
 
 
 def moe_mx_dequantize(format, elements, scales, x, stream=None):
     """The values of block-scaled ``elements`` and ``scales`` into bf16 ``x [rows, cols]``."""
-    import torch
-    rows, cols = _matrix("x", x)
-    dev, u8 = x.device, torch.uint8
-    _on(dev, stream, lib().moe_mx_dequantize, rows, cols, format,
-        _take(dev, "elements", elements, u8, rows, mx_elements_per_row(format, cols)),
-        _take(dev, "scales", scales, u8, rows, cols // 32), _take(dev, "x", x, torch.bfloat16, rows, cols))
-
-
-def _bytes(device, name, t, n):
-    """Pointer of a contiguous uint8 tensor of at least n values (any shape)."""
-    import torch
-    if t is None:
-        _refuse(f"{name} is missing")
-    if t.dtype is not torch.uint8 or t.numel() < n or t.device != device or not t.is_contiguous():
-        _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}; "
-                f"expected {n} contiguous uint8 values on {device}")
-    return t.data_ptr()
-
-
-def _ws(device, ws):
-    """(pointer, bytes) of a workspace."""
-    if ws is None:
-        return None, 0
-    return _bytes(device, "ws", ws, 0), ws.numel()
+    rows, cols, dev = _matrix("x", x)
+    _on(dev, stream, _lib.moe_mx_dequantize, rows, cols, format,
+        _take(dev, "elements", elements, _u8, rows, mx_elements_per_row(format, cols)),
+        _take(dev, "scales", scales, _u8, rows, cols // 32), _take(dev, "x", x, _bf16, rows, cols))
 
 
 def moe_mx_grouped_ffn(sh, format, x_q, x_scales, offsets, w13_q, w13_scales, w2_q, w2_scales, y_perm, ws, stream=None):
     """``x_q`` / ``x_scales`` and ``y_perm`` have ``sh.capacity`` rows."""
-    import torch
-    dev, d, F, El = x_q.device, sh.d, sh.F, sh.E_local
-    cap = sh.capacity
-    _on(dev, stream, lib().moe_mx_grouped_ffn, ctypes.byref(shape_c(sh)), format,
+    d, F, El, cap = sh.d, sh.F, sh.E_local, sh.capacity
+    dev = _matrix("y_perm", y_perm)[2]
+    _on(dev, stream, _lib.moe_mx_grouped_ffn, ctypes.byref(shape_c(sh)), format,
         _bytes(dev, "x_q", x_q, cap * mx_elements_per_row(format, d)), _bytes(dev, "x_scales", x_scales, cap * (d // 32)),
-        _take(dev, "offsets", offsets, torch.int32, El if sh.expert_capacity > 0 else El + 1),
-        _bytes(dev, "w13_q", w13_q, El * 2 * F * d // 2), _bytes(dev, "w13_scales", w13_scales, El * 2 * F * (d // 32)),
+        _take(dev, "offsets", offsets, _i32, El if sh.expert_capacity > 0 else El + 1),
+        _bytes(dev, "w13_q", w13_q, El * F * d), _bytes(dev, "w13_scales", w13_scales, El * 2 * F * (d // 32)),
         _bytes(dev, "w2_q", w2_q, El * d * F // 2), _bytes(dev, "w2_scales", w2_scales, El * d * (F // 32)),
-        _take(dev, "y_perm", y_perm, torch.bfloat16, cap, d), *_ws(dev, ws))
+        _take(dev, "y_perm", y_perm, _bf16, cap, d), *_ws(dev, ws))
 
 
 def moe_add_rmsnorm(x, residual, gamma, eps, h, y, y_q=None, y_scales=None, rstd=None, stream=None):
-    import torch
-    rows, d = _matrix("x", x)
-    dev, bf, u8 = x.device, torch.bfloat16, torch.uint8
-
-    def opt(name, t, dtype, *shape):
-        return None if t is None else _take(dev, name, t, dtype, *shape)
-
-    _on(dev, stream, lib().moe_add_rmsnorm, rows, d, eps, _take(dev, "x", x, bf, rows, d),
-        opt("residual", residual, bf, rows, d), _take(dev, "gamma", gamma, bf, d), opt("h", h, bf, rows, d),
-        opt("y", y, bf, rows, d), opt("y_q", y_q, u8, rows, d), opt("y_scales", y_scales, u8, rows, d // 32),
-        opt("rstd", rstd, torch.float32, rows))
+    rows, d, dev = _matrix("x", x)
+    _on(dev, stream, _lib.moe_add_rmsnorm, rows, d, eps, _take(dev, "x", x, _bf16, rows, d),
+        None if residual is None else _take(dev, "residual", residual, _bf16, rows, d), _take(dev, "gamma", gamma, _bf16, d),
+        None if h is None else _take(dev, "h", h, _bf16, rows, d), None if y is None else _take(dev, "y", y, _bf16, rows, d),
+        None if y_q is None else _take(dev, "y_q", y_q, _u8, rows, d),
+        None if y_scales is None else _take(dev, "y_scales", y_scales, _u8, rows, d // 32),
+        None if rstd is None else _take(dev, "rstd", rstd, _f32, rows))
 
 
 def moe_add_rmsnorm_backward(dy, dh, h, gamma, rstd, dx, dgamma, ws, stream=None):
-    import torch
-    rows, d = _matrix("dy", dy)
-    dev, bf = dy.device, torch.bfloat16
-    _on(dev, stream, lib().moe_add_rmsnorm_backward, rows, d, _take(dev, "dy", dy, bf, rows, d),
-        None if dh is None else _take(dev, "dh", dh, bf, rows, d), _take(dev, "h", h, bf, rows, d),
-        _take(dev, "gamma", gamma, bf, d), _take(dev, "rstd", rstd, torch.float32, rows),
-        _take(dev, "dx", dx, bf, rows, d), _take(dev, "dgamma", dgamma, bf, d), *_ws(dev, ws))
+    rows, d, dev = _matrix("dy", dy)
+    _on(dev, stream, _lib.moe_add_rmsnorm_backward, rows, d, _take(dev, "dy", dy, _bf16, rows, d),
+        None if dh is None else _take(dev, "dh", dh, _bf16, rows, d), _take(dev, "h", h, _bf16, rows, d),
+        _take(dev, "gamma", gamma, _bf16, d), _take(dev, "rstd", rstd, _f32, rows),
+        _take(dev, "dx", dx, _bf16, rows, d), _take(dev, "dgamma", dgamma, _bf16, d), *_ws(dev, ws))
 
 
 def add_rmsnorm_workspace_size(rows: int, d: int) -> int:
@@ -340,28 +338,23 @@ def alloc_add_rmsnorm_workspace(rows: int, d: int, device="cuda"):
 def moe_layer_decode(sh, x, w_router, bias, w13, w2, ws13, ws2, out, ws, scales=None, stream=None):
     """``scales``: None with bf16 weights, or (w13_scales, w2_scales, ws13_scales, ws2_scales) with e2m1 ones
     (the last two None without a shared expert)."""
-    import torch
-    dev, bf = x.device, torch.bfloat16
     T, d, F, Fs, El = sh.T, sh.d, sh.F, sh.F_shared, sh.E_local
+    dev = _matrix("x", x)[2]
+    s = scales if scales is not None else (None,) * 4
 
     def weights(name, t, s, rows, K):
-        if t is None:
-            _refuse(f"{name} is missing")
-        if scales is None:
-            if t.dtype is not bf or t.numel() != rows * K or t.device != dev or not t.is_contiguous():
-                _refuse(f"{name} is {t.dtype} {tuple(t.shape)} on {t.device}; expected {rows * K} contiguous {bf} "
-                        f"values on {dev}")
-            return t.data_ptr(), None
-        return _bytes(dev, name, t, rows * K // 2), _bytes(dev, name + "_scales", s, rows * (K // 32))
+        if scales is not None:
+            return _bytes(dev, name, t, rows * K // 2), _bytes(dev, name + "_scales", s, rows * (K // 32))
+        if t is None or t.dtype is not _bf16 or t.numel() != rows * K or t.device != dev or not t.is_contiguous():
+            _mismatch(dev, name, t, _bf16, f"of {rows * K} values")
+        return t.data_ptr(), None
 
-    s = scales if scales is not None else (None,) * 4
     none = (None, None)
-    _on(dev, stream, lib().moe_layer_decode, ctypes.byref(shape_c(sh)), _take(dev, "x", x, bf, T, d),
-        _take(dev, "w_router", w_router, bf, sh.E, d),
-        None if bias is None else _take(dev, "bias", bias, torch.float32, sh.E),
+    _on(dev, stream, _lib.moe_layer_decode, ctypes.byref(shape_c(sh)), _take(dev, "x", x, _bf16, T, d),
+        _take(dev, "w_router", w_router, _bf16, sh.E, d), None if bias is None else _take(dev, "bias", bias, _f32, sh.E),
         *weights("w13", w13, s[0], El * 2 * F, d), *weights("w2", w2, s[1], El * d, F),
         *(weights("ws13", ws13, s[2], 2 * Fs, d) if Fs else none), *(weights("ws2", ws2, s[3], d, Fs) if Fs else none),
-        _take(dev, "out", out, bf, T, d), *_ws(dev, ws))
+        _take(dev, "out", out, _bf16, T, d), *_ws(dev, ws))
 
 
 # ---------------------------------------------------------------------------------------

@@ -118,7 +118,7 @@ def mlp64(x, w13, w2, fmt):
 REL = 5e-3
 
 
-def run_mlp(fmt, d, F, counts, capacity=0, seed=0, whole=True):
+def run_mlp(fmt, d, F, counts, capacity=0, seed=0):
     """Runs the MLP on experts of `counts` rows; compares every live row, and that no other row was written."""
     rng = np.random.default_rng(seed)
     E = len(counts)
@@ -144,12 +144,6 @@ def run_mlp(fmt, d, F, counts, capacity=0, seed=0, whole=True):
     ws = moe.alloc_workspace(sh, moe.MOE_WS_MX_FFN)
     off = dev(np.asarray(counts, np.int32) if capacity else offsets)
     x_q, x_s = dev(mx.pack(x_codes, fmt)), dev(x_scales)
-    if not whole:                       # scales that start at an odd address
-        def odd(t):
-            b = torch.empty(t.numel() + 1, dtype=U8, device="cuda")
-            b[1:] = t.flatten()
-            return b[1:]
-        x_s, s13, s2 = odd(x_s), odd(s13), odd(s2)
     moe.moe_mx_grouped_ffn(sh, fmt, x_q, x_s, off, w13, s13, w2, s2, y, ws)
     got = y.double().cpu().numpy()
     assert (got[~live] == -77.0).all()
@@ -186,10 +180,9 @@ def test_mlp_capacity_layout(fmt, capacity, counts):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_mlp_many_experts_and_odd_scale_addresses(fmt):
+def test_mlp_many_experts(fmt):
     rng = np.random.default_rng(3)
     run_mlp(fmt, 64, 64, rng.integers(0, 4, 300).tolist())
-    run_mlp(fmt, 256, 128, [5, 300, 0, 33], whole=False)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
