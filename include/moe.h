@@ -378,7 +378,7 @@ int moe_mx_dequantize(int64_t rows, int32_t cols, int format, const void* elemen
  *    w13_q, w13_scales  [E_local * 2F, d]    E2M1, the rows as in w13
  *    w2_q, w2_scales    [E_local * d, F]     E2M1, the rows as in w2
  *    y_perm             [cap, d] bf16; rows outside every segment are not written
- * Limits beside moe_grouped_ffn's: d and F multiples of 32.  Offsets, layouts and clamping as there.
+ * Limits beside moe_grouped_ffn's: d and F multiples of 32, d * F < 2^31.  Offsets, layouts and clamping as there.
  * ws: MOE_WS_MX_FFN bytes. */
 int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, const void* x_scales,
                        const int32_t* offsets, const void* w13_q, const void* w13_scales, const void* w2_q,

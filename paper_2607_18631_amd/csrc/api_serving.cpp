@@ -89,6 +89,8 @@ int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, co
   CHECK(check_mx_shape(shape));
   if (shape->E_local > moe::kMaxGroups)
     return fail(MOE_ERR_UNSUPPORTED, "E_local (%d) > %d", shape->E_local, moe::kMaxGroups);
+  if ((int64_t)shape->d * shape->F >= moe::kMxGroupValues)
+    return fail(MOE_ERR_UNSUPPORTED, "d * F (%lld) >= 2^31", (long long)shape->d * shape->F);
   if (shape->T == 0) return ok();
   CHECK(check_ptr(x_q, 16, "x_q"));
   CHECK(check_ptr(x_scales, 16, "x_scales"));

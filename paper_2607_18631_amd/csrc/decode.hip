@@ -421,7 +421,7 @@ __global__ __launch_bounds__(64 * kWaves, MX ? 4 : 3) void k_decode_up(DecodePro
   product<MX, WHOLE, 2>(o, split, g.room, lds, [&](int slot, int f, const f32x4 (&s)[2]) {
     float v[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = s[0][j] / (1.0f + expf(-s[0][j])) * s[1][j];
+    for (int j = 0; j < 4; ++j) v[j] = s[0][j] * __builtin_amdgcn_rcpf(1.0f + __expf(-s[0][j])) * s[1][j];
     const u32x2 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
     *reinterpret_cast<u32x2*>(act + (int64_t)slot * o.features + f) = w;
   });

@@ -2,10 +2,15 @@
 // e2m1, on v_mfma_scale_f32_32x32x64_f8f6f4 (elements multiplied as they are, each block of 32 products
 // times both blocks' powers of two, float32 accumulation).
 //
-// A workgroup owns BM rows of one group and BN weight rows; its K loop runs over slices of 128 values
-// held in a ring of LDS stages, filled by direct-to-LDS copies that are issued STAGES - 1 slices ahead.
-// Each wave multiplies MT x 2 tiles of 32 x 32: the weights are the first operand, so that a lane holds
-// 16 of the 32 output features of one row, its partner lane (l ^ 32) the others.
+// A workgroup owns BM rows of one group and BN weight rows; its K loop runs over slices of 128 values in
+// a ring of LDS stages, filled by direct-to-LDS copies.  Each wave multiplies MT x 2 tiles of 32 x 32: the
+// weights are the first operand, so that a lane holds 16 of the 32 output features of one row, its partner
+// lane (l ^ 32) the others.
+//
+// The matrix cores are not to wait for LDS: a slice is multiplied in two halves of 64 values, each half's
+// operands being read from LDS while the half before it is multiplied.  The one barrier of a slice stands
+// between its halves.  There the whole slice is in registers, so its stage is free and takes the copies of
+// the slice STAGES further on; STAGES - 1 slices are on their way or landed.
 //
 // SwiGLU: a wave's two weight tiles are the gate and the up rows of the same 32 features, so the
 // activation and the maximum of its block are formed in registers, and the block leaves as elements and
@@ -14,6 +19,8 @@
 // Operand layout of the instruction (lane l: row l % 32, half q = l / 32): e2m1 holds k = 32 q + j in
 // nibble j; e4m3 holds k = 16 q + j in bytes j < 16 and k = 32 + 16 q + (j - 16) in the others; the scale
 // given by lane l is that of block q of its row for either.
+#include <algorithm>
+
 #include "common.hpp"
 #include "gemm_device.hpp"
 #include "kernels.hpp"
@@ -24,18 +31,16 @@ namespace {
 
 constexpr int kSlice = 128;            // K values per stage
 
-// 4-byte direct-to-LDS copy, as dma16_v
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void dma4_v(const void* src, void* dst) {
-  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(char*)dst;
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds) : "memory", "m0");
+// a 4-bit operand: 16 bytes of the 32 that the instruction's type has room for
+__device__ __forceinline__ i32x8 narrow(u32x4 v) {
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  const i32x4 w = __builtin_bit_cast(i32x4, v);
+  return __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
 }
-#pragma clang diagnostic pop
 
-template <int FMT, int WM, int WN, int MT, int STAGES_>
+template <int FMT, int WM, int WN, int MT, int MOST_STAGES>
 struct MxTile {
-  static constexpr int F = FMT, M_WAVES = WM, N_WAVES = WN, M_TILES = MT, STAGES = STAGES_;
+  static constexpr int F = FMT, M_WAVES = WM, N_WAVES = WN, M_TILES = MT;
   static constexpr int WAVES = WM * WN;
   static constexpr int NTH = WAVES * 64;
   static constexpr int BM = WM * MT * 32;
@@ -43,12 +48,19 @@ struct MxTile {
   static constexpr int XROW = FMT == MX_E4M3 ? 128 : 64;      // bytes of a slice's row
   static constexpr int X_BYTES = BM * XROW;
   static constexpr int W_BYTES = BN * 64;
-  static constexpr int S_BYTES = (BM + BN + 63) / 64 * 256;   // scales: 4 blocks per row
-  static constexpr int STAGE = X_BYTES + W_BYTES + S_BYTES;
-  static constexpr int LDS = STAGE * STAGES;
-  static constexpr int NX = X_BYTES / 1024, NW = W_BYTES / 1024, NS = S_BYTES / 256;   // wave copies
+  static constexpr int STAGE = X_BYTES + W_BYTES;
+  // the scales of 4 slices: 16 bytes per row (of X, then of W), two sets of them
+  static constexpr int SROWS = (BM + BN + 63) / 64 * 64;
+  static constexpr int FIT = (160 * 1024 - 2 * SROWS * 16) / STAGE;
+  static constexpr int STAGES = FIT < MOST_STAGES ? FIT : MOST_STAGES;
+  static constexpr int LDS = STAGE * STAGES + 2 * SROWS * 16;
+  static constexpr int NX = X_BYTES / 1024, NW = W_BYTES / 1024, NS = SROWS / 64;   // wave copies
+  // the same workgroup for a group's last rows, where fewer than BM are left
+  template <int FEWER>
+  using Low = MxTile<FMT, WM, WN, FEWER, MOST_STAGES>;
   static_assert(X_BYTES % 1024 == 0 && W_BYTES % 1024 == 0, "whole wave copies");
-  static constexpr int COPIES = NX + NW + NS;
+  static_assert(STAGES >= 3, "two slices on their way beside the one in use");
+  static_assert(STAGES <= 5, "the scales of slice s + STAGES replace those of 8 slices before");
 };
 
 // 16-byte chunk of a row where the stage holds the row's chunk c: rows that share a bank cycle take
@@ -59,195 +71,234 @@ __device__ __forceinline__ int mx_chunk(int row, int c) {
   return c ^ ((row / RPG) % CPR);
 }
 
+// rows row0 .. row0 + rows of group g (1 <= rows <= BM), output features feat0 ..
 template <class T, bool SWIGLU, bool WHOLE>
-__global__ __launch_bounds__(T::NTH) void k_mx_gemm(MxGemmProblem p) {
-  extern __shared__ __align__(16) char smem[];
-  __shared__ int s_tmp[T::WAVES];
-  __shared__ int s_own[4];
+__device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int g, int64_t row0, int rows, int feat0) {
   constexpr int FMT = T::F, MT = T::M_TILES;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int K = p.K, N = p.N;
-  constexpr int FEAT = SWIGLU ? T::BN / 2 : T::BN;             // output features of a tile
-  const int ntiles = (N + FEAT - 1) / FEAT;
 
-  // ---- this workgroup's tile: groups in order, inside a group m fastest ----
-  // rows of group g, clamped to the buffers
-  auto segment = [&](int g, int64_t& a, int64_t& b) {
-    if (p.seg_stride > 0) {
-      a = (int64_t)g * p.seg_stride;
-      b = a + min(max(p.offsets[g], 0), p.seg_stride);
-    } else {
-      a = min(max((int64_t)p.offsets[g], (int64_t)0), p.max_rows);
-      b = max(a, min((int64_t)p.offsets[g + 1], p.max_rows));
-    }
-  };
-  constexpr int GPT = (kMaxGroups + T::NTH - 1) / T::NTH;
-  int mt[GPT], sum = 0;
-#pragma unroll
-  for (int i = 0; i < GPT; ++i) {
-    const int g = tid * GPT + i;
-    mt[i] = 0;
-    if (g < p.groups) {
-      int64_t a, b;
-      segment(g, a, b);
-      mt[i] = (int)((b - a + T::BM - 1) / T::BM);
-    }
-    sum += mt[i];
-  }
-  int excl;
-  const int total = block_exclusive_scan<T::NTH>(sum, s_tmp, excl);
-  // consecutive tiles to one XCD (workgroup b runs on XCD b % 8): they share weights and rows in its L2
-  const int64_t tiles = (int64_t)total * ntiles;
-  const int64_t per = (tiles + 7) / 8;
-  const int64_t slot = blockIdx.x / 8;
-  const int64_t tile = (int64_t)(blockIdx.x % 8) * per + slot;
-  if (slot >= per || tile >= tiles) return;                    // the whole workgroup
-#pragma unroll
-  for (int i = 0; i < GPT; ++i) {
-    const int64_t first = (int64_t)excl * ntiles, last = (int64_t)(excl + mt[i]) * ntiles;
-    if (tile >= first && tile < last) {
-      s_own[0] = tid * GPT + i;
-      s_own[1] = (int)((tile - first) % mt[i]);
-      s_own[2] = (int)((tile - first) / mt[i]);
-    }
-    excl += mt[i];
-  }
-  __syncthreads();
-  const int g = __builtin_amdgcn_readfirstlane(s_own[0]);
-  const int tm = __builtin_amdgcn_readfirstlane(s_own[1]);
-  const int tn = __builtin_amdgcn_readfirstlane(s_own[2]);
-  int64_t seg_a, seg_b;
-  segment(g, seg_a, seg_b);
-  const int64_t row0 = seg_a + (int64_t)tm * T::BM;
-  const int rows = (int)min((int64_t)T::BM, seg_b - row0);     // live rows, >= 1
-  const int feat0 = tn * FEAT;
-
-  // ---- slice copies ----
+  // ---- where the copies come from ----
   const int KB = K / 32;                                       // blocks of a row
   const int nk = (K + kSlice - 1) / kSlice;
-  const int64_t wrow0 = (int64_t)g * (SWIGLU ? 2 * (int64_t)N : N);
   const int64_t xbytes = FMT == MX_E4M3 ? K : K / 2, wbytes = K / 2;
-  // weight row (of the group) of the stage's row i: plain, or per wave 32 gate and 32 up rows
-  auto weight_row = [&](int i) -> int64_t {
+  // Each wave's share of a stage: copies wave, wave + WAVES, ... of the token rows and the weights.  A lane's source is
+  // a base of the wave's plus `from` bytes, 32 bits wide: the host admits no larger group.
+  constexpr int MINE = (T::NX + T::NW + T::WAVES - 1) / T::WAVES, LEAST = (T::NX + T::NW) / T::WAVES;
+  constexpr int SMINE = (T::NS + T::WAVES - 1) / T::WAVES;
+  uint32_t from[MINE];
+  int kofs[MINE];                                              // first K value of a copy
+  const char* sfrom[SMINE];
+  const int64_t wrow0 = (int64_t)g * (SWIGLU ? 2 * (int64_t)N : N);
+  // weight row (from the group's first) of the stage's row i: plain, or per wave 32 gate and 32 up rows
+  auto weight_row = [&](int i) -> uint32_t {
     if constexpr (SWIGLU) {
       const int f = min(feat0 + (i / 64) * 32 + (i & 31), N - 1);
-      return wrow0 + ((i & 32) ? N + f : f);
+      return (i & 32) ? N + f : f;
     } else {
-      return wrow0 + min(feat0 + i, N - 1);
+      return min(feat0 + i, N - 1);
     }
   };
-  // each wave's share of a stage: copies wave, wave + WAVES, ... of the token rows, the weights and the
-  // scales; the sources of slice 0, which move by the same step each slice
-  constexpr int MINE = (T::COPIES + T::WAVES - 1) / T::WAVES;
-  const char* src[MINE];
-  int kofs[MINE];                                              // first K value (copies of 16 bytes) or block
+  const char* xb = (const char*)p.X + row0 * xbytes;
+  const char* wb = (const char*)p.W + wrow0 * wbytes;
+  const char* xs = (const char*)p.X_scales + row0 * KB;
+  const char* ws = (const char*)p.W_scales + wrow0 * KB;
 #pragma unroll
   for (int c = 0; c < MINE; ++c) {
     const int id = wave + c * T::WAVES;
-    src[c] = nullptr;
-    kofs[c] = 0;
     if (id < T::NX) {
       const int byte = id * 1024 + lane * 16, r = byte / T::XROW, ch = mx_chunk<T::XROW>(r, (byte % T::XROW) / 16);
-      src[c] = (const char*)p.X + (row0 + min(r, rows - 1)) * xbytes + ch * 16;
+      from[c] = (uint32_t)(min(r, rows - 1) * xbytes) + ch * 16;
       kofs[c] = ch * (FMT == MX_E4M3 ? 16 : 32);
-    } else if (id < T::NX + T::NW) {
-      const int byte = (id - T::NX) * 1024 + lane * 16, r = byte / 64, ch = mx_chunk<64>(r, (byte % 64) / 16);
-      src[c] = (const char*)p.W + weight_row(r) * wbytes + ch * 16;
+    } else {
+      const int byte = (min(id, T::NX + T::NW - 1) - T::NX) * 1024 + lane * 16, r = byte / 64;
+      const int ch = mx_chunk<64>(r, (byte % 64) / 16);
+      from[c] = (uint32_t)(weight_row(r) * wbytes) + ch * 16;
       kofs[c] = ch * 32;
-    } else if (id < T::COPIES) {
-      const int r = (id - T::NX - T::NW) * 64 + lane;          // rows of X, then of W (and a few more)
-      src[c] = r < T::BM ? (const char*)p.X_scales + (row0 + min(r, rows - 1)) * KB
-                         : (const char*)p.W_scales + weight_row(r - T::BM) * KB;
     }
   }
-  auto stage = [&](int s, int ring) {
-    char* base = smem + ring * T::STAGE;
+#pragma unroll
+  for (int c = 0; c < SMINE; ++c) {
+    const int r = (wave + c * T::WAVES) * 64 + lane;
+    sfrom[c] = r < T::BM ? xs + (int64_t)min(r, rows - 1) * KB : ws + (int64_t)weight_row(min(r - T::BM, T::BN - 1)) * KB;
+  }
+  // Scales: a row's 4 bytes of one slice are as many cache accesses and requests as its 64 or 128 bytes of values, so
+  // they come for 4 slices at a time: 16 bytes per row.  Where rows end inside the last group's 16 bytes, it starts
+  // that much earlier.  (WHOLE rows have 16 scales at least.)
+  char* s_scales = smem + T::STAGES * T::STAGE;
+  auto group_start = [&](int s) { return WHOLE ? min(s / 4 * 16, KB - 16) : s / 4 * 16; };   // block
+  // part 0 .. MT - 1 of a stage's copies
+  auto stage_part = [&](int s, char* base, int part) {
 #pragma unroll
     for (int c = 0; c < MINE; ++c) {
+      if (c % MT != part) continue;
       const int id = wave + c * T::WAVES;                      // wave-uniform
-      if (id < T::NX + T::NW) {
-        const bool x = id < T::NX;
-        const int64_t step = x ? (FMT == MX_E4M3 ? 128 : 64) : 64;
-        const char* q = src[c] + s * step;
-        if constexpr (!WHOLE) {
-          if (s * kSlice + kofs[c] >= K) q = (const char*)g_zero_chunk;
-        }
-        dma16_v(q, (bf16_t*)(base + id * 1024));
-      } else if (id < T::COPIES) {
-        char* dst = base + T::X_BYTES + T::W_BYTES + (id - T::NX - T::NW) * 256;
-        if constexpr (WHOLE) {
-          dma4_v(src[c] + s * 4, dst);
-        } else {
-          // scales past the row's end are zeros, never the next row's bytes (255 would make NaN of zeros)
-          uint32_t v = 0;
+      if (c >= LEAST && id >= T::NX + T::NW) continue;
+      const bool x = id < T::NX;
+      const char* b = x ? xb + s * (FMT == MX_E4M3 ? 128 : 64) : wb + s * 64;
+      bf16_t* dst = (bf16_t*)(base + id * 1024);
+      if constexpr (WHOLE) {
+        dma16_sv(b, from[c], dst);
+      } else {
+        dma16_v(s * kSlice + kofs[c] < K ? b + from[c] : (const char*)g_zero_chunk, dst);
+      }
+    }
+    if (part == MT - 1 && s % 4 == 0) {
+      char* set = s_scales + s / 4 % 2 * (T::SROWS * 16);
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (s * 4 + j < KB) v |= (uint32_t)(uint8_t)src[c][s * 4 + j] << (8 * j);
-          *reinterpret_cast<uint32_t*>(dst + lane * 4) = v;
+      for (int c = 0; c < SMINE; ++c) {
+        const int id = wave + c * T::WAVES;
+        if (id < T::NS) {
+          if constexpr (WHOLE) {
+            dma16_v(sfrom[c] + group_start(s), (bf16_t*)(set + id * 1024));
+          } else {
+            // scales past the row's end are zeros, never the next row's bytes (255 would make NaN of zeros)
+            u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (s * 4 + j < KB) v[j / 4] |= (uint32_t)(uint8_t)sfrom[c][s * 4 + j] << (8 * (j % 4));
+            *reinterpret_cast<u32x4*>(set + id * 1024 + lane * 16) = v;
+          }
         }
       }
     }
   };
+  auto stage = [&](int s, char* base) {
+#pragma unroll
+    for (int part = 0; part < MT; ++part) stage_part(s, base, part);
+  };
 
   // ---- K loop ----
-  // copies that every wave issues per stage at least: the wait counts by these
-  constexpr int PER_WAVE = (WHOLE ? T::COPIES : T::NX + T::NW) / T::WAVES;
+  // the values' copies of the stages that may be on their way (the scales' come on top of them now and then: the wait
+  // then asks for a little more than it has to)
+  constexpr int AHEAD = (T::STAGES - 2) * LEAST;
   const int wm = wave / T::N_WAVES, wn = wave % T::N_WAVES;
   const int r = lane & 31, q = lane >> 5;
   f32x16 acc[2][MT];
+
+  struct Half {                        // operands of 64 values of K
+    i32x8 w[2], x[MT];
+  };
+  struct Scales {
+    int w[2], x[MT];                   // a slice's 4 blocks; shifted by the lane's q, bytes 0 and 2 are its own of the two halves
+  };
+  const int wrow = wn * 64 + r, xrow = wm * MT * 32 + r;
+  auto read_w = [&](const char* base, int j, Half& h) {
+    const char* W = base + T::X_BYTES + wrow * 64 + mx_chunk<64>(wrow, 2 * j + q) * 16;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) h.w[n] = narrow(ld16(W + n * 32 * 64));
+  };
+  auto read_x = [&](const char* base, int j, int m, Half& h) {
+    if constexpr (FMT == MX_E4M3) {
+      const char* lo = base + xrow * 128 + mx_chunk<128>(xrow, 4 * j + q) * 16;
+      const char* hi = base + xrow * 128 + mx_chunk<128>(xrow, 4 * j + 2 + q) * 16;
+      const u32x4 a = ld16(lo + m * 32 * 128), b = ld16(hi + m * 32 * 128);
+      h.x[m] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+    } else {
+      const char* X = base + xrow * 64 + mx_chunk<64>(xrow, 2 * j + q) * 16;
+      h.x[m] = narrow(ld16(X + m * 32 * 64));
+    }
+  };
+  auto read_scales = [&](int i, Scales& s) {                     // of slice i
+    const char* S = s_scales + i / 4 % 2 * (T::SROWS * 16) + (4 * i - group_start(i));
+#pragma unroll
+    for (int n = 0; n < 2; ++n) s.w[n] = *reinterpret_cast<const int*>(S + (T::BM + wrow + n * 32) * 16);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) s.x[m] = *reinterpret_cast<const int*>(S + (xrow + m * 32) * 16);
+  };
+  // (apart from the read: a shift beside it would wait for it, and for the half read before it)
+  auto own_scales = [&](const Scales& all, Scales& s) {
+#pragma unroll
+    for (int n = 0; n < 2; ++n) s.w[n] = (uint32_t)all.w[n] >> (8 * q);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) s.x[m] = (uint32_t)all.x[m] >> (8 * q);
+  };
+  // One half's products (16 per wave and more than twice as many cycles of the matrix core as LDS needs for the next
+  // half's operands), with the wave's other work between them: an instruction waits for those before it, so reads or
+  // copies in one piece would leave the matrix core idle until the last of all eight waves' had been issued.  `other(m)`
+  // is issued behind the products of tile m, all reads before the last tile's.
+  // (Matrix instructions are no memory accesses to the compiler, which would move them all behind the barrier.  The empty
+  // statement that claims to change their results keeps them where they stand.)
+  auto multiply = [&](auto jc, const Half& h, const Scales& s, auto other) {
+    constexpr int j = decltype(jc)::value;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+        acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(h.w[n], h.x[m], acc[n][m], 4, FMT == MX_E4M3 ? 0 : 4,
+                                                                    2 * j, s.w[n], 2 * j, s.x[m]);
+      asm volatile("" : "+v"(acc[0][m]), "+v"(acc[1][m]));
+      __builtin_amdgcn_sched_barrier(0);
+      other(m);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // the next half's operands: the weights and the first tile's rows, then the other tiles'
+  auto read_part = [&](const char* base, int j, int m, Half& h) {
+    if (m == 0) {
+      read_w(base, j, h);
+      read_x(base, j, 0, h);
+    }
+    constexpr int EACH = MT > 2 ? (MT - 1 + MT - 3) / (MT - 2) : 1;
+#pragma unroll
+    for (int t = 1; t < MT; ++t)
+      if ((MT > 2 ? 1 + (t - 1) / EACH : 0) == m) read_x(base, j, t, h);
+  };
+  constexpr std::integral_constant<int, 0> first{};
+  constexpr std::integral_constant<int, 1> second{};
+
+  char* ring[T::STAGES];
+#pragma unroll
+  for (int s = 0; s < T::STAGES; ++s) ring[s] = smem + s * T::STAGE;
+  auto rotate = [&] {
+    char* f = ring[0];
+#pragma unroll
+    for (int s = 0; s + 1 < T::STAGES; ++s) ring[s] = ring[s + 1];
+    ring[T::STAGES - 1] = f;
+  };
+#pragma unroll
+  for (int s = 0; s < T::STAGES; ++s)
+    if (s < nk) stage(s, ring[s]);
 #pragma unroll
   for (int n = 0; n < 2; ++n)
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.f;
-
+  if (nk >= T::STAGES) wait_vmcnt<AHEAD + LEAST>();
+  else wait_vmcnt<0>();
+  lds_barrier();
+  Half a, b;
+  Scales s0, s1;
 #pragma unroll
-  for (int s = 0; s < T::STAGES - 1; ++s)
-    if (s < nk) stage(s, s);
-  int ring = 0;
-  for (int s = 0; s < nk; ++s) {
-    // slice s has landed once at most the copies of the slices behind it are in flight
-    if (s + T::STAGES - 1 <= nk) wait_vmcnt<(T::STAGES - 2) * PER_WAVE>();
-    else wait_vmcnt<0>();
-    lds_barrier();                     // every wave's copies, and its reads of the stage filled next
-    if (s + T::STAGES - 1 < nk) stage(s + T::STAGES - 1, ring == 0 ? T::STAGES - 1 : ring - 1);
-    const char* X = smem + ring * T::STAGE;
-    const char* W = X + T::X_BYTES;
-    const uint32_t* S = reinterpret_cast<const uint32_t*>(W + T::W_BYTES);
-    int sx[MT], sw[2];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) sx[m] = (int)(S[(wm * MT + m) * 32 + r] >> (8 * q));
-#pragma unroll
-    for (int n = 0; n < 2; ++n) sw[n] = (int)(S[T::BM + wn * 64 + n * 32 + r] >> (8 * q));
-    static_for<2>([&](auto jc) {
-      constexpr int j = decltype(jc)::value;
-      i32x8 w[2];
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int row = wn * 64 + n * 32 + r;
-        const u32x4 v = ld16(W + row * 64 + mx_chunk<64>(row, 2 * j + q) * 16);
-        w[n] = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-      }
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const int row = (wm * MT + m) * 32 + r;
-        i32x8 x;
-        if constexpr (FMT == MX_E4M3) {
-          const u32x4 lo = ld16(X + row * 128 + mx_chunk<128>(row, 4 * j + q) * 16);
-          const u32x4 hi = ld16(X + row * 128 + mx_chunk<128>(row, 4 * j + 2 + q) * 16);
-          x = i32x8{(int)lo[0], (int)lo[1], (int)lo[2], (int)lo[3], (int)hi[0], (int)hi[1], (int)hi[2], (int)hi[3]};
-        } else {
-          const u32x4 v = ld16(X + row * 64 + mx_chunk<64>(row, 2 * j + q) * 16);
-          x = i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0};
-        }
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-          acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w[n], x, acc[n][m], 4, FMT == MX_E4M3 ? 0 : 4,
-                                                                      2 * j, sw[n], 2 * j, sx[m]);
-      }
+  for (int m = 0; m < MT; ++m) read_part(ring[0], 0, m, a);
+  read_scales(0, s1);
+  own_scales(s1, s0);
+  // ring[0] holds slice s, ring[1] the next, ...
+  int s = 0;
+  for (; s + T::STAGES < nk; ++s) {
+    multiply(first, a, s0, [&](int m) { read_part(ring[0], 1, m, b); });
+    wait_vmcnt<AHEAD>();               // slice s + 1: at most the copies of those behind it are in flight
+    lds_barrier();                     // every wave's, and its reads of slice s
+    multiply(second, b, s0, [&](int m) {
+      read_part(ring[1], 0, m, a);
+      if (m == 0) read_scales(s + 1, s1);
+      stage_part(s + T::STAGES, ring[0], m);
     });
-    ring = ring == T::STAGES - 1 ? 0 : ring + 1;
+    own_scales(s1, s0);
+    rotate();
+  }
+  for (; s < nk; ++s) {                // the last slices: nothing to copy
+    multiply(first, a, s0, [&](int m) { read_part(ring[0], 1, m, b); });
+    wait_vmcnt<0>();
+    lds_barrier();
+    multiply(second, b, s0, [&](int m) {
+      read_part(ring[1], 0, m, a);     // (behind the last slice: what lies there, not used)
+      if (m == 0) read_scales(min(s + 1, nk - 1), s1);
+    });
+    own_scales(s1, s0);
+    rotate();
   }
 
   // ---- results: lane (r, q) holds features 8 g + 4 q + i (g, i < 4) of row r of each tile ----
@@ -261,7 +312,7 @@ __global__ __launch_bounds__(T::NTH) void k_mx_gemm(MxGemmProblem p) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float h = acc[0][m][i], u = acc[1][m][i];
-        a[i] = h / (1.0f + expf(-h)) * u;
+        a[i] = h * __builtin_amdgcn_rcpf(1.0f + __expf(-h)) * u;
       }
       uint32_t most = abs_max_bits(a);
       most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
@@ -324,25 +375,98 @@ __global__ __launch_bounds__(T::NTH) void k_mx_gemm(MxGemmProblem p) {
 }
 
 template <class T, bool SWIGLU, bool WHOLE>
+__global__ __launch_bounds__(T::NTH) void k_mx_gemm(MxGemmProblem p) {
+  extern __shared__ __align__(16) char smem[];
+  const int lane = threadIdx.x & 63;
+  constexpr int FEAT = SWIGLU ? T::BN / 2 : T::BN;             // output features of a tile
+  const int ntiles = (p.N + FEAT - 1) / FEAT;
+
+  // Tiles: groups in order, inside a group m fastest.  Every wave finds its own, a group per lane: the launch cannot
+  // know the loads, and what precedes a tile's first copy is time that the compute unit idles.
+  struct Block {                                               // of up to 64 groups
+    int64_t row0;                                              // this lane's group: rows, clamped to the buffers
+    int rows, tiles, upto;                                     // (upto: tiles of the block's groups up to this one)
+  };
+  auto load = [&](int base) {
+    const int g = base + lane;
+    Block k = {0, 0, 0, 0};
+    if (g < p.groups) {
+      if (p.seg_stride > 0) {
+        k.row0 = (int64_t)g * p.seg_stride;
+        k.rows = min(max(p.offsets[g], 0), p.seg_stride);
+      } else {
+        const int64_t a = p.offsets[g], b = p.offsets[g + 1];
+        k.row0 = min(max(a, (int64_t)0), p.max_rows);
+        k.rows = (int)(max(k.row0, min(b, p.max_rows)) - k.row0);
+      }
+    }
+    k.tiles = k.upto = (int)(((int64_t)k.rows + T::BM - 1) / T::BM);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int n = __shfl_up(k.upto, o, 64);
+      if (lane >= o) k.upto += n;
+    }
+    return k;
+  };
+  Block k = load(0);
+  int total = __builtin_amdgcn_readlane(k.upto, 63);
+  for (int base = 64; base < p.groups; base += 64) total += __builtin_amdgcn_readlane(load(base).upto, 63);
+  // consecutive tiles to one XCD (workgroup b runs on XCD b % 8): they share weights and rows in its L2
+  const uint32_t tiles = (uint32_t)total * ntiles, per = (tiles + 7) / 8;   // (the host bounds it by the grid)
+  const uint32_t slot = blockIdx.x / 8, tile = blockIdx.x % 8 * per + slot;
+  if (slot >= per || tile >= tiles) return;                    // the whole workgroup
+  const int at = (int)(tile / ntiles);
+  int before = 0, base = 0;
+  uint64_t mask;
+  while (!(mask = __ballot(at < before + k.upto))) {           // (at < total: some block has it)
+    before += __builtin_amdgcn_readlane(k.upto, 63);
+    k = load(base += 64);
+  }
+  const int l = __builtin_ctzll(mask), g = base + l;
+  const int mine = __builtin_amdgcn_readlane(k.tiles, l);
+  before += __builtin_amdgcn_readlane(k.upto, l) - mine;
+  const int local = (int)(tile - (uint32_t)before * ntiles), m0 = local % mine * T::BM;
+  const int64_t row0 = (((int64_t)__builtin_amdgcn_readlane((int)(k.row0 >> 32), l) << 32) |
+                        (uint32_t)__builtin_amdgcn_readlane((int)k.row0, l)) + m0;
+  const int rows = min(T::BM, __builtin_amdgcn_readlane(k.rows, l) - m0);   // >= 1
+  const int feat0 = local / mine * FEAT;
+  // a group's last rows: as many of a wave's tiles as they need
+  constexpr int MT = T::M_TILES;
+  if constexpr (MT > 1) {
+    using Low = typename T::template Low<1>;
+    static_assert(Low::LDS <= T::LDS, "within the launch's LDS");
+    if (rows <= Low::BM) return mx_tile<Low, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
+  }
+  if constexpr (MT > 2) {
+    using Low = typename T::template Low<2>;
+    static_assert(Low::LDS <= T::LDS, "within the launch's LDS");
+    if (rows <= Low::BM) return mx_tile<Low, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
+  }
+  mx_tile<T, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
+}
+
+template <class T, bool SWIGLU, bool WHOLE>
 hipError_t launch_as(const MxGemmProblem& p, hipStream_t stream) {
   static OccCache cache;
   hipError_t err = hipSuccess;
   const void* fn = reinterpret_cast<const void*>(&k_mx_gemm<T, SWIGLU, WHOLE>);
-  if (kernel_occupancy(cache, fn, T::NTH, T::LDS, err) <= 0) return err;
+  const int per_cu = kernel_occupancy(cache, fn, T::NTH, T::LDS, err);
+  if (per_cu <= 0) return err;
   constexpr int FEAT = SWIGLU ? T::BN / 2 : T::BN;
   const int64_t ntiles = (p.N + FEAT - 1) / FEAT;
   // every group adds at most one partial tile
   int64_t mtiles = p.max_rows / T::BM + (p.groups < p.max_rows ? p.groups : p.max_rows);
   if (p.seg_stride > 0) mtiles = (int64_t)p.groups * ((p.seg_stride + T::BM - 1) / T::BM);
-  const int64_t blocks = (mtiles * ntiles + 7) / 8 * 8;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t blocks = (mtiles * ntiles + 7) / 8 * 8;        // whole rounds of the 8 XCDs
+  if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_mx_gemm<T, SWIGLU, WHOLE>), dim3((unsigned)blocks), dim3(T::NTH), T::LDS, stream, p);
   return hipGetLastError();
 }
 
 template <class T>
 hipError_t launch_tile(const MxGemmProblem& p, hipStream_t stream) {
-  const bool whole = p.K % kSlice == 0;    // no slice has a row's end inside
+  // no slice has a row's end inside, and a row has the scales of a group
+  const bool whole = p.K % kSlice == 0 && p.K >= 4 * kSlice;
   if (p.swiglu) return whole ? launch_as<T, true, true>(p, stream) : launch_as<T, true, false>(p, stream);
   return whole ? launch_as<T, false, true>(p, stream) : launch_as<T, false, false>(p, stream);
 }
@@ -350,15 +474,16 @@ hipError_t launch_tile(const MxGemmProblem& p, hipStream_t stream) {
 template <int FMT>
 hipError_t launch_format(const MxGemmProblem& p, hipStream_t stream) {
   const int64_t per_group = p.max_rows / p.groups;             // the rows themselves stay on the device
-  if (per_group > 128) return launch_tile<MxTile<FMT, 2, 4, 4, 3>>(p, stream);
-  if (per_group > 32) return launch_tile<MxTile<FMT, 2, 4, 2, 3>>(p, stream);
+  if (per_group > 128) return launch_tile<MxTile<FMT, 2, 4, 4, 4>>(p, stream);
+  if (per_group > 32) return launch_tile<MxTile<FMT, 2, 4, 2, 4>>(p, stream);
   return launch_tile<MxTile<FMT, 1, 4, 1, 4>>(p, stream);
 }
 
 }  // namespace
 
 hipError_t launch_mx_gemm(const MxGemmProblem& p, hipStream_t stream) {
-  if (p.groups < 1 || p.groups > kMaxGroups || p.K % 32 || p.N % 32) return hipErrorInvalidValue;
+  if (p.groups < 1 || p.groups > kMaxGroups || p.K % 32 || p.N % 32 || (int64_t)p.N * p.K >= kMxGroupValues)
+    return hipErrorInvalidValue;
   return p.format == MX_E4M3 ? launch_format<MX_E4M3>(p, stream) : launch_format<MX_E2M1>(p, stream);
 }
 
