@@ -19,7 +19,6 @@
 // Operand layout of the instruction (lane l: row l % 32, half q = l / 32): e2m1 holds k = 32 q + j in
 // nibble j; e4m3 holds k = 16 q + j in bytes j < 16 and k = 32 + 16 q + (j - 16) in the others; the scale
 // given by lane l is that of block q of its row for either.
-#include <algorithm>
 
 #include "common.hpp"
 #include "gemm_device.hpp"
@@ -29,8 +28,6 @@
 namespace moe {
 namespace {
 
-constexpr int kSlice = 128;            // K values per stage
-
 // a 4-bit operand: 16 bytes of the 32 that the instruction's type has room for
 __device__ __forceinline__ i32x8 narrow(u32x4 v) {
   typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -38,18 +35,22 @@ __device__ __forceinline__ i32x8 narrow(u32x4 v) {
   return __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
 }
 
-template <int FMT, int WM, int WN, int MT, int MOST_STAGES>
+// a slice: KS values of K
+template <int FMT, int WM, int WN, int MT, int MOST_STAGES, int KS>
 struct MxTile {
   static constexpr int F = FMT, M_WAVES = WM, N_WAVES = WN, M_TILES = MT;
   static constexpr int WAVES = WM * WN;
   static constexpr int NTH = WAVES * 64;
   static constexpr int BM = WM * MT * 32;
   static constexpr int BN = WN * 64;                          // weight rows
-  static constexpr int XROW = FMT == MX_E4M3 ? 128 : 64;      // bytes of a slice's row
+  static constexpr int SLICE = KS, PARTS = KS / 64;           // (a part: what one instruction takes)
+  static constexpr int XROW = FMT == MX_E4M3 ? KS : KS / 2;   // bytes of a slice's row
+  static constexpr int WROW = KS / 2;
   static constexpr int X_BYTES = BM * XROW;
-  static constexpr int W_BYTES = BN * 64;
+  static constexpr int W_BYTES = BN * WROW;
   static constexpr int STAGE = X_BYTES + W_BYTES;
-  // the scales of 4 slices: 16 bytes per row (of X, then of W), two sets of them
+  // the scales of 512 values: 16 bytes per row (of X, then of W), two sets of them
+  static constexpr int GROUP = 512 / KS;                      // slices
   static constexpr int SROWS = (BM + BN + 63) / 64 * 64;
   static constexpr int FIT = (160 * 1024 - 2 * SROWS * 16) / STAGE;
   static constexpr int STAGES = FIT < MOST_STAGES ? FIT : MOST_STAGES;
@@ -57,10 +58,11 @@ struct MxTile {
   static constexpr int NX = X_BYTES / 1024, NW = W_BYTES / 1024, NS = SROWS / 64;   // wave copies
   // the same workgroup for a group's last rows, where fewer than BM are left
   template <int FEWER>
-  using Low = MxTile<FMT, WM, WN, FEWER, MOST_STAGES>;
+  using Low = MxTile<FMT, WM, WN, FEWER, MOST_STAGES, KS>;
   static_assert(X_BYTES % 1024 == 0 && W_BYTES % 1024 == 0, "whole wave copies");
-  static_assert(STAGES >= 3, "two slices on their way beside the one in use");
-  static_assert(STAGES <= 5, "the scales of slice s + STAGES replace those of 8 slices before");
+  static_assert(STAGES >= 2, "a slice on its way beside the one in use");
+  static_assert(STAGES <= GROUP + 1, "the scales of slice s + STAGES replace those of two groups before");
+  static_assert(PARTS % 2 == 0, "a slice begins in the first of two operand buffers");
 };
 
 // 16-byte chunk of a row where the stage holds the row's chunk c: rows that share a bank cycle take
@@ -80,7 +82,7 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
 
   // ---- where the copies come from ----
   const int KB = K / 32;                                       // blocks of a row
-  const int nk = (K + kSlice - 1) / kSlice;
+  const int nk = (K + T::SLICE - 1) / T::SLICE;
   const int64_t xbytes = FMT == MX_E4M3 ? K : K / 2, wbytes = K / 2;
   // Each wave's share of a stage: copies wave, wave + WAVES, ... of the token rows and the weights.  A lane's source is
   // a base of the wave's plus `from` bytes, 32 bits wide: the host admits no larger group.
@@ -111,8 +113,8 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
       from[c] = (uint32_t)(min(r, rows - 1) * xbytes) + ch * 16;
       kofs[c] = ch * (FMT == MX_E4M3 ? 16 : 32);
     } else {
-      const int byte = (min(id, T::NX + T::NW - 1) - T::NX) * 1024 + lane * 16, r = byte / 64;
-      const int ch = mx_chunk<64>(r, (byte % 64) / 16);
+      const int byte = (min(id, T::NX + T::NW - 1) - T::NX) * 1024 + lane * 16, r = byte / T::WROW;
+      const int ch = mx_chunk<T::WROW>(r, (byte % T::WROW) / 16);
       from[c] = (uint32_t)(weight_row(r) * wbytes) + ch * 16;
       kofs[c] = ch * 32;
     }
@@ -123,10 +125,10 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     sfrom[c] = r < T::BM ? xs + (int64_t)min(r, rows - 1) * KB : ws + (int64_t)weight_row(min(r - T::BM, T::BN - 1)) * KB;
   }
   // Scales: a row's 4 bytes of one slice are as many cache accesses and requests as its 64 or 128 bytes of values, so
-  // they come for 4 slices at a time: 16 bytes per row.  Where rows end inside the last group's 16 bytes, it starts
+  // they come for 512 values at a time: 16 bytes per row.  Where rows end inside the last group's 16 bytes, it starts
   // that much earlier.  (WHOLE rows have 16 scales at least.)
   char* s_scales = smem + T::STAGES * T::STAGE;
-  auto group_start = [&](int s) { return WHOLE ? min(s / 4 * 16, KB - 16) : s / 4 * 16; };   // block
+  auto group_start = [&](int s) { return WHOLE ? min(s / T::GROUP * 16, KB - 16) : s / T::GROUP * 16; };   // block
   // part 0 .. MT - 1 of a stage's copies
   auto stage_part = [&](int s, char* base, int part) {
 #pragma unroll
@@ -135,16 +137,16 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
       const int id = wave + c * T::WAVES;                      // wave-uniform
       if (c >= LEAST && id >= T::NX + T::NW) continue;
       const bool x = id < T::NX;
-      const char* b = x ? xb + s * (FMT == MX_E4M3 ? 128 : 64) : wb + s * 64;
+      const char* b = x ? xb + s * T::XROW : wb + s * T::WROW;
       bf16_t* dst = (bf16_t*)(base + id * 1024);
       if constexpr (WHOLE) {
         dma16_sv(b, from[c], dst);
       } else {
-        dma16_v(s * kSlice + kofs[c] < K ? b + from[c] : (const char*)g_zero_chunk, dst);
+        dma16_v(s * T::SLICE + kofs[c] < K ? b + from[c] : (const char*)g_zero_chunk, dst);
       }
     }
-    if (part == MT - 1 && s % 4 == 0) {
-      char* set = s_scales + s / 4 % 2 * (T::SROWS * 16);
+    if (part == MT - 1 && s % T::GROUP == 0) {
+      char* set = s_scales + s / T::GROUP % 2 * (T::SROWS * 16);
 #pragma unroll
       for (int c = 0; c < SMINE; ++c) {
         const int id = wave + c * T::WAVES;
@@ -156,7 +158,7 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
             u32x4 v = {0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < 16; ++j)
-              if (s * 4 + j < KB) v[j / 4] |= (uint32_t)(uint8_t)sfrom[c][s * 4 + j] << (8 * (j % 4));
+              if (group_start(s) + j < KB) v[j / 4] |= (uint32_t)(uint8_t)sfrom[c][group_start(s) + j] << (8 * (j % 4));
             *reinterpret_cast<u32x4*>(set + id * 1024 + lane * 16) = v;
           }
         }
@@ -176,37 +178,37 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   const int r = lane & 31, q = lane >> 5;
   f32x16 acc[2][MT];
 
-  struct Half {                        // operands of 64 values of K
+  struct Part {                        // operands of 64 values of K
     i32x8 w[2], x[MT];
   };
-  struct Scales {
-    int w[2], x[MT];                   // a slice's 4 blocks; shifted by the lane's q, bytes 0 and 2 are its own of the two halves
+  struct Scales {                      // of two parts: 4 blocks; shifted by the lane's q, bytes 0 and 2 are its own
+    int w[2], x[MT];
   };
   const int wrow = wn * 64 + r, xrow = wm * MT * 32 + r;
-  auto read_w = [&](const char* base, int j, Half& h) {
-    const char* W = base + T::X_BYTES + wrow * 64 + mx_chunk<64>(wrow, 2 * j + q) * 16;
+  auto read_w = [&](const char* base, int j, Part& h) {
+    const char* W = base + T::X_BYTES + wrow * T::WROW + mx_chunk<T::WROW>(wrow, 2 * j + q) * 16;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) h.w[n] = narrow(ld16(W + n * 32 * 64));
+    for (int n = 0; n < 2; ++n) h.w[n] = narrow(ld16(W + n * 32 * T::WROW));
   };
-  auto read_x = [&](const char* base, int j, int m, Half& h) {
+  auto read_x = [&](const char* base, int j, int m, Part& h) {
     if constexpr (FMT == MX_E4M3) {
-      const char* lo = base + xrow * 128 + mx_chunk<128>(xrow, 4 * j + q) * 16;
-      const char* hi = base + xrow * 128 + mx_chunk<128>(xrow, 4 * j + 2 + q) * 16;
-      const u32x4 a = ld16(lo + m * 32 * 128), b = ld16(hi + m * 32 * 128);
+      const char* lo = base + xrow * T::XROW + mx_chunk<T::XROW>(xrow, 4 * j + q) * 16;
+      const char* hi = base + xrow * T::XROW + mx_chunk<T::XROW>(xrow, 4 * j + 2 + q) * 16;
+      const u32x4 a = ld16(lo + m * 32 * T::XROW), b = ld16(hi + m * 32 * T::XROW);
       h.x[m] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
     } else {
-      const char* X = base + xrow * 64 + mx_chunk<64>(xrow, 2 * j + q) * 16;
-      h.x[m] = narrow(ld16(X + m * 32 * 64));
+      const char* X = base + xrow * T::XROW + mx_chunk<T::XROW>(xrow, 2 * j + q) * 16;
+      h.x[m] = narrow(ld16(X + m * 32 * T::XROW));
     }
   };
-  auto read_scales = [&](int i, Scales& s) {                     // of slice i
-    const char* S = s_scales + i / 4 % 2 * (T::SROWS * 16) + (4 * i - group_start(i));
+  auto read_scales = [&](int i, int j, Scales& s) {              // of slice i, parts j and j + 1
+    const char* S = s_scales + i / T::GROUP % 2 * (T::SROWS * 16) + (T::SLICE / 32 * i - group_start(i)) + 2 * j;
 #pragma unroll
     for (int n = 0; n < 2; ++n) s.w[n] = *reinterpret_cast<const int*>(S + (T::BM + wrow + n * 32) * 16);
 #pragma unroll
     for (int m = 0; m < MT; ++m) s.x[m] = *reinterpret_cast<const int*>(S + (xrow + m * 32) * 16);
   };
-  // (apart from the read: a shift beside it would wait for it, and for the half read before it)
+  // (apart from the read: a shift beside it would wait for it, and for the operands read before it)
   auto own_scales = [&](const Scales& all, Scales& s) {
 #pragma unroll
     for (int n = 0; n < 2; ++n) s.w[n] = (uint32_t)all.w[n] >> (8 * q);
@@ -219,7 +221,7 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   // is issued behind the products of tile m, all reads before the last tile's.
   // (Matrix instructions are no memory accesses to the compiler, which would move them all behind the barrier.  The empty
   // statement that claims to change their results keeps them where they stand.)
-  auto multiply = [&](auto jc, const Half& h, const Scales& s, auto other) {
+  auto multiply = [&](auto jc, const Part& h, const Scales& s, auto other) {
     constexpr int j = decltype(jc)::value;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -227,7 +229,7 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
 #pragma unroll
       for (int n = 0; n < 2; ++n)
         acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(h.w[n], h.x[m], acc[n][m], 4, FMT == MX_E4M3 ? 0 : 4,
-                                                                    2 * j, s.w[n], 2 * j, s.x[m]);
+                                                                    2 * (j % 2), s.w[n], 2 * (j % 2), s.x[m]);
       asm volatile("" : "+v"(acc[0][m]), "+v"(acc[1][m]));
       __builtin_amdgcn_sched_barrier(0);
       other(m);
@@ -235,7 +237,7 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     }
   };
   // the next half's operands: the weights and the first tile's rows, then the other tiles'
-  auto read_part = [&](const char* base, int j, int m, Half& h) {
+  auto read_part = [&](const char* base, int j, int m, Part& h) {
     if (m == 0) {
       read_w(base, j, h);
       read_x(base, j, 0, h);
@@ -245,8 +247,6 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     for (int t = 1; t < MT; ++t)
       if ((MT > 2 ? 1 + (t - 1) / EACH : 0) == m) read_x(base, j, t, h);
   };
-  constexpr std::integral_constant<int, 0> first{};
-  constexpr std::integral_constant<int, 1> second{};
 
   char* ring[T::STAGES];
 #pragma unroll
@@ -269,33 +269,50 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   if (nk >= T::STAGES) wait_vmcnt<AHEAD + LEAST>();
   else wait_vmcnt<0>();
   lds_barrier();
-  Half a, b;
+  Part part[2];
   Scales s0, s1;
 #pragma unroll
-  for (int m = 0; m < MT; ++m) read_part(ring[0], 0, m, a);
-  read_scales(0, s1);
+  for (int m = 0; m < MT; ++m) read_part(ring[0], 0, m, part[0]);
+  read_scales(0, 0, s1);
   own_scales(s1, s0);
   // ring[0] holds slice s, ring[1] the next, ...
   int s = 0;
+  // all parts of a slice but the last
+  auto most_parts = [&] {
+    auto one = [&](auto jc) {
+      constexpr int j = decltype(jc)::value;
+      multiply(jc, part[j % 2], s0, [&](int m) {
+        read_part(ring[0], j + 1, m, part[(j + 1) % 2]);
+        if (j % 2 && m == 0) read_scales(s, j + 1, s1);
+      });
+      if (j % 2) own_scales(s1, s0);
+    };
+    one(std::integral_constant<int, 0>{});
+    if constexpr (T::PARTS > 2) {
+      one(std::integral_constant<int, 1>{});
+      one(std::integral_constant<int, 2>{});
+    }
+  };
+  constexpr std::integral_constant<int, T::PARTS - 1> last{};
   for (; s + T::STAGES < nk; ++s) {
-    multiply(first, a, s0, [&](int m) { read_part(ring[0], 1, m, b); });
+    most_parts();
     wait_vmcnt<AHEAD>();               // slice s + 1: at most the copies of those behind it are in flight
     lds_barrier();                     // every wave's, and its reads of slice s
-    multiply(second, b, s0, [&](int m) {
-      read_part(ring[1], 0, m, a);
-      if (m == 0) read_scales(s + 1, s1);
+    multiply(last, part[1], s0, [&](int m) {
+      read_part(ring[1], 0, m, part[0]);
+      if (m == 0) read_scales(s + 1, 0, s1);
       stage_part(s + T::STAGES, ring[0], m);
     });
     own_scales(s1, s0);
     rotate();
   }
   for (; s < nk; ++s) {                // the last slices: nothing to copy
-    multiply(first, a, s0, [&](int m) { read_part(ring[0], 1, m, b); });
+    most_parts();
     wait_vmcnt<0>();
     lds_barrier();
-    multiply(second, b, s0, [&](int m) {
-      read_part(ring[1], 0, m, a);     // (behind the last slice: what lies there, not used)
-      if (m == 0) read_scales(min(s + 1, nk - 1), s1);
+    multiply(last, part[1], s0, [&](int m) {
+      read_part(ring[1], 0, m, part[0]);   // (behind the last slice: what lies there, not used)
+      if (m == 0) read_scales(min(s + 1, nk - 1), 0, s1);
     });
     own_scales(s1, s0);
     rotate();
@@ -434,15 +451,22 @@ __global__ __launch_bounds__(T::NTH) void k_mx_gemm(MxGemmProblem p) {
   constexpr int MT = T::M_TILES;
   if constexpr (MT > 1) {
     using Low = typename T::template Low<1>;
-    static_assert(Low::LDS <= T::LDS, "within the launch's LDS");
     if (rows <= Low::BM) return mx_tile<Low, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
   }
   if constexpr (MT > 2) {
     using Low = typename T::template Low<2>;
-    static_assert(Low::LDS <= T::LDS, "within the launch's LDS");
     if (rows <= Low::BM) return mx_tile<Low, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
   }
   mx_tile<T, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
+}
+
+// a launch holds the tile and its low ones
+template <class T>
+constexpr int launch_lds() {
+  int most = T::LDS;
+  if (T::M_TILES > 1 && T::template Low<1>::LDS > most) most = T::template Low<1>::LDS;
+  if (T::M_TILES > 2 && T::template Low<2>::LDS > most) most = T::template Low<2>::LDS;
+  return most;
 }
 
 template <class T, bool SWIGLU, bool WHOLE>
@@ -450,7 +474,7 @@ hipError_t launch_as(const MxGemmProblem& p, hipStream_t stream) {
   static OccCache cache;
   hipError_t err = hipSuccess;
   const void* fn = reinterpret_cast<const void*>(&k_mx_gemm<T, SWIGLU, WHOLE>);
-  const int per_cu = kernel_occupancy(cache, fn, T::NTH, T::LDS, err);
+  const int per_cu = kernel_occupancy(cache, fn, T::NTH, launch_lds<T>(), err);
   if (per_cu <= 0) return err;
   constexpr int FEAT = SWIGLU ? T::BN / 2 : T::BN;
   const int64_t ntiles = (p.N + FEAT - 1) / FEAT;
@@ -459,24 +483,42 @@ hipError_t launch_as(const MxGemmProblem& p, hipStream_t stream) {
   if (p.seg_stride > 0) mtiles = (int64_t)p.groups * ((p.seg_stride + T::BM - 1) / T::BM);
   const int64_t blocks = (mtiles * ntiles + 7) / 8 * 8;        // whole rounds of the 8 XCDs
   if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((k_mx_gemm<T, SWIGLU, WHOLE>), dim3((unsigned)blocks), dim3(T::NTH), T::LDS, stream, p);
+  hipLaunchKernelGGL((k_mx_gemm<T, SWIGLU, WHOLE>), dim3((unsigned)blocks), dim3(T::NTH), launch_lds<T>(), stream, p);
   return hipGetLastError();
 }
 
-template <class T>
-hipError_t launch_tile(const MxGemmProblem& p, hipStream_t stream) {
-  // no slice has a row's end inside, and a row has the scales of a group
-  const bool whole = p.K % kSlice == 0 && p.K >= 4 * kSlice;
+// Slices of 256 values where the token rows are e2m1 and every slice is whole: rows of 128 bytes are one cache line
+// each, rows of 64 cost as many accesses for half the bytes (2048 rows on 8 experts of 4096 x 14336: 395 us a call
+// against 444; 8192 rows: 841 against 874).  e4m3 rows have 128 bytes in slices of 128, and LDS has no room for two
+// such stages of 256 rows.
+template <int FMT, int MT>
+hipError_t launch_rows(const MxGemmProblem& p, hipStream_t stream) {
+  if constexpr (FMT == MX_E2M1) {
+    if (p.K % 256 == 0 && p.K >= 512) {
+      using T = MxTile<FMT, 2, 4, MT, 3, 256>;
+      return p.swiglu ? launch_as<T, true, true>(p, stream) : launch_as<T, false, true>(p, stream);
+    }
+  }
+  // whole: no slice has a row's end inside, and a row has the scales of a group
+  using T = MxTile<FMT, 2, 4, MT, 4, 128>;
+  const bool whole = p.K % 128 == 0 && p.K >= 512;
   if (p.swiglu) return whole ? launch_as<T, true, true>(p, stream) : launch_as<T, true, false>(p, stream);
   return whole ? launch_as<T, false, true>(p, stream) : launch_as<T, false, false>(p, stream);
 }
 
+// Tiles of 256 rows where the groups have more than 64 rows in the mean (the loads themselves stay on the device) and
+// the tiles fill the chip, of 128 rows elsewhere.  256 rows read the weights once for a group's 130 rows: 8192 rows on 64
+// experts of 2048 x 1408 in e2m1 120 us a call against 149; 2048 rows on 8 of 4096 x 14336 373 against 395.  Tiles of 128
+// are twice as many: 2048 rows on 4 of 2048 x 1024 in e4m3 35 against 51, 501 on 8 of 2048 x 1408 33 against 49; and with
+// few rows a group's low tile has more slices on their way (512 rows on 32 of 7168 x 2048 in e2m1 153 against 168).
+// (Tiles of 32 rows with 4 waves were slower than the low tile of 64: 160 in the last case; and 128 x 128 with 4 waves
+// slower than 128 x 256, however few: 43 against 33 for the 501 rows.)
 template <int FMT>
 hipError_t launch_format(const MxGemmProblem& p, hipStream_t stream) {
-  const int64_t per_group = p.max_rows / p.groups;             // the rows themselves stay on the device
-  if (per_group > 128) return launch_tile<MxTile<FMT, 2, 4, 4, 4>>(p, stream);
-  if (per_group > 32) return launch_tile<MxTile<FMT, 2, 4, 2, 4>>(p, stream);
-  return launch_tile<MxTile<FMT, 1, 4, 1, 4>>(p, stream);
+  const int64_t per_group = p.max_rows / p.groups;
+  const int64_t weight_rows = (int64_t)p.N * (p.swiglu ? 2 : 1);
+  const int64_t tiles = p.groups * ((per_group + 255) / 256) * ((weight_rows + 255) / 256);
+  return per_group > 64 && tiles >= cu_count() ? launch_rows<FMT, 4>(p, stream) : launch_rows<FMT, 2>(p, stream);
 }
 
 }  // namespace

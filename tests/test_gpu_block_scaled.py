@@ -174,6 +174,17 @@ def test_mlp_rows(fmt, counts):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d,F", [(1024, 512), (1152, 640), (1056, 544)])
+def test_mlp_enough_rows_to_fill_the_chip(fmt, d, F):
+    """64 experts of 70 rows in the mean, from none to more than a tile of 256; K of whole slices of 256, of 128,
+    and neither."""
+    counts = [300, 257, 0, 1, 64, 65, 128, 129, 191, 192, 255, 256]
+    counts += [(4480 - sum(counts)) // 52 + (i % 3 - 1) * 20 for i in range(52)]
+    assert sum(counts) > 64 * 64
+    run_mlp(fmt, d, F, counts, seed=d)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("capacity,counts", [(4, [0, 3, 4, 9]), (48, [48, 50, 1]), (160, [160, 7, 0, 159])])
 def test_mlp_capacity_layout(fmt, capacity, counts):
     run_mlp(fmt, 256, 320, counts, capacity=capacity)
