@@ -378,7 +378,8 @@ int moe_mx_dequantize(int64_t rows, int32_t cols, int format, const void* elemen
  *    w13_q, w13_scales  [E_local * 2F, d]    E2M1, the rows as in w13
  *    w2_q, w2_scales    [E_local * d, F]     E2M1, the rows as in w2
  *    y_perm             [cap, d] bf16; rows outside every segment are not written
- * Limits beside moe_grouped_ffn's: d and F multiples of 32, d * F < 2^31.  Offsets, layouts and clamping as there.
+ * Limits beside moe_grouped_ffn's: d and F multiples of 32 below 2^20, d * F < 2^31.  Offsets, layouts
+ * and clamping as there.
  * ws: MOE_WS_MX_FFN bytes. */
 int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, const void* x_scales,
                        const int32_t* offsets, const void* w13_q, const void* w13_scales, const void* w2_q,
@@ -416,9 +417,10 @@ size_t moe_add_rmsnorm_workspace_size(int64_t rows, int32_t d);
  * The weights are bf16 (every *_scales NULL) or E2M1 (every one given): then w13, w2, ws13 and ws2 are
  * the elements, their values enter the products exactly, and x and the activation stay bf16.  Either
  * way the router and x are bf16.  Honours expert_capacity; ignores fusion.
- * d, F and F_shared are below 2^20; with E2M1 they are multiples of 32, d <= 16384 and F, F_shared <= 32768.  The chosen experts and their gates are left at
- * the start of the workspace, at the offsets moe_workspace_offset gives for MOE_REGION_TOPK_IDX and
- * MOE_REGION_TOPK_W.  Deterministic.  Calls that may overlap need a workspace each.
+ * d, F and F_shared are below 2^20; with E2M1 they are multiples of 32, d <= 16384 and F, F_shared <=
+ * 32768.  The chosen experts and their gates are left at the start of the workspace, at the offsets
+ * moe_workspace_offset gives for MOE_REGION_TOPK_IDX and MOE_REGION_TOPK_W.  Deterministic.  Calls that
+ * may overlap need a workspace each.
  * ws: MOE_WS_DECODE bytes. */
 int moe_layer_decode(const moe_shape_t* shape, const void* x, const void* w_router, const float* bias,
                      const void* w13, const void* w13_scales, const void* w2, const void* w2_scales,

@@ -89,6 +89,9 @@ int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, co
   CHECK(check_mx_shape(shape));
   if (shape->E_local > moe::kMaxGroups)
     return fail(MOE_ERR_UNSUPPORTED, "E_local (%d) > %d", shape->E_local, moe::kMaxGroups);
+  // 32-bit byte offsets into a tile's 256 rows and into a group's weights
+  const int32_t widest = shape->d > shape->F ? shape->d : shape->F;
+  if (widest >= moe::kMxRowValues) return fail(MOE_ERR_UNSUPPORTED, "d or F (%d) >= 2^20", widest);
   if ((int64_t)shape->d * shape->F >= moe::kMxGroupValues)
     return fail(MOE_ERR_UNSUPPORTED, "d * F (%lld) >= 2^31", (long long)shape->d * shape->F);
   if (shape->T == 0) return ok();

@@ -330,7 +330,9 @@ struct MxGemmProblem {
   uint8_t* Yq;                // swiglu: elements [rows, N]
   uint8_t* Y_scales;          // swiglu: scales [rows, N / 32]
 };
-constexpr int64_t kMxGroupValues = int64_t(1) << 31;   // N * K stays below: 32-bit offsets inside a group's weights
+// N * K, N and K stay below: 32-bit offsets inside a group's weights and inside a tile's rows
+constexpr int64_t kMxGroupValues = int64_t(1) << 31;
+constexpr int32_t kMxRowValues = 1 << 20;
 hipError_t launch_mx_gemm(const MxGemmProblem& p, hipStream_t stream);
 
 // Few-token layer: at most kDecodeTokens tokens, so the tokens of an expert are a 64-bit mask.

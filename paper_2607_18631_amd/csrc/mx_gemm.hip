@@ -482,7 +482,7 @@ hipError_t launch_as(const MxGemmProblem& p, hipStream_t stream) {
   int64_t mtiles = p.max_rows / T::BM + (p.groups < p.max_rows ? p.groups : p.max_rows);
   if (p.seg_stride > 0) mtiles = (int64_t)p.groups * ((p.seg_stride + T::BM - 1) / T::BM);
   const int64_t blocks = (mtiles * ntiles + 7) / 8 * 8;        // whole rounds of the 8 XCDs
-  if (blocks > INT32_MAX) return hipErrorInvalidConfiguration;
+  if (blocks * T::NTH > UINT32_MAX) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((k_mx_gemm<T, SWIGLU, WHOLE>), dim3((unsigned)blocks), dim3(T::NTH), launch_lds<T>(), stream, p);
   return hipGetLastError();
 }
@@ -524,7 +524,8 @@ hipError_t launch_format(const MxGemmProblem& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_mx_gemm(const MxGemmProblem& p, hipStream_t stream) {
-  if (p.groups < 1 || p.groups > kMaxGroups || p.K % 32 || p.N % 32 || (int64_t)p.N * p.K >= kMxGroupValues)
+  if (p.groups < 1 || p.groups > kMaxGroups || p.K % 32 || p.N % 32 || (int64_t)p.N * p.K >= kMxGroupValues ||
+      p.N >= kMxRowValues || p.K >= kMxRowValues)
     return hipErrorInvalidValue;
   return p.format == MX_E4M3 ? launch_format<MX_E4M3>(p, stream) : launch_format<MX_E2M1>(p, stream);
 }
