@@ -491,34 +491,39 @@ hipError_t launch_as(const MxGemmProblem& p, hipStream_t stream) {
 // each, rows of 64 cost as many accesses for half the bytes (2048 rows on 8 experts of 4096 x 14336: 395 us a call
 // against 444; 8192 rows: 841 against 874).  e4m3 rows have 128 bytes in slices of 128, and LDS has no room for two
 // such stages of 256 rows.
-template <int FMT, int MT>
-hipError_t launch_rows(const MxGemmProblem& p, hipStream_t stream) {
-  if constexpr (FMT == MX_E2M1) {
+template <int FMT, int WM, int WN, int MT>
+hipError_t launch_tile(const MxGemmProblem& p, hipStream_t stream) {
+  if constexpr (FMT == MX_E2M1 && WN == 4) {
     if (p.K % 256 == 0 && p.K >= 512) {
-      using T = MxTile<FMT, 2, 4, MT, 3, 256>;
+      using T = MxTile<FMT, WM, WN, MT, 3, 256>;
       return p.swiglu ? launch_as<T, true, true>(p, stream) : launch_as<T, false, true>(p, stream);
     }
   }
   // whole: no slice has a row's end inside, and a row has the scales of a group
-  using T = MxTile<FMT, 2, 4, MT, 4, 128>;
+  using T = MxTile<FMT, WM, WN, MT, 4, 128>;
   const bool whole = p.K % 128 == 0 && p.K >= 512;
   if (p.swiglu) return whole ? launch_as<T, true, true>(p, stream) : launch_as<T, true, false>(p, stream);
   return whole ? launch_as<T, false, true>(p, stream) : launch_as<T, false, false>(p, stream);
 }
 
-// Tiles of 256 rows where the groups have more than 64 rows in the mean (the loads themselves stay on the device) and
-// the tiles fill the chip, of 128 rows elsewhere.  256 rows read the weights once for a group's 130 rows: 8192 rows on 64
-// experts of 2048 x 1408 in e2m1 120 us a call against 149; 2048 rows on 8 of 4096 x 14336 373 against 395.  Tiles of 128
-// are twice as many: 2048 rows on 4 of 2048 x 1024 in e4m3 35 against 51, 501 on 8 of 2048 x 1408 33 against 49; and with
-// few rows a group's low tile has more slices on their way (512 rows on 32 of 7168 x 2048 in e2m1 153 against 168).
-// (Tiles of 32 rows with 4 waves were slower than the low tile of 64: 160 in the last case; and 128 x 128 with 4 waves
-// slower than 128 x 256, however few: 43 against 33 for the 501 rows.)
+// Rows x weight rows of a tile, by the rows that a group has in the mean (the loads themselves stay on the device):
+//   256 x 256  where groups have more than 64 rows and the tiles fill the chip.  The weights are read once for a group's
+//              130 rows: 8192 rows on 64 experts of 2048 x 1408 in e2m1 120 us a call against 149 with 128 rows.
+//   128 x 128  where such tiles fit on the chip at once: a tile waits for its slices' latency, so more compute units
+//              asking is more memory at work.  501 rows on 8 experts of 2048 x 1408 in e4m3 26 us against 32 with
+//              128 x 256; but 2048 rows on 4 of 2048 x 1024, which take a second round, 45 against 35.
+//   128 x 256  elsewhere: that case 35 us against 51 with 256 rows; 512 rows on 32 experts of 7168 x 2048 in e2m1 153
+//              against 168, as a low tile of 64 rows has more slices on their way.
+// (Slower everywhere: 32 and 64 rows with 4 waves, which have nobody on their SIMD to multiply while they read.)
 template <int FMT>
 hipError_t launch_format(const MxGemmProblem& p, hipStream_t stream) {
   const int64_t per_group = p.max_rows / p.groups;
-  const int64_t weight_rows = (int64_t)p.N * (p.swiglu ? 2 : 1);
-  const int64_t tiles = p.groups * ((per_group + 255) / 256) * ((weight_rows + 255) / 256);
-  return per_group > 64 && tiles >= cu_count() ? launch_rows<FMT, 4>(p, stream) : launch_rows<FMT, 2>(p, stream);
+  const int64_t weight_rows = (int64_t)p.N * (p.swiglu ? 2 : 1), chip = cu_count();
+  // (a group ends half a tile early in the mean)
+  const int64_t narrow = p.groups * ((per_group + 64 + 127) / 128) * ((weight_rows + 127) / 128);
+  const int64_t large = p.groups * ((per_group + 255) / 256) * ((weight_rows + 255) / 256);
+  if (narrow <= chip) return launch_tile<FMT, 4, 2, 1>(p, stream);
+  return per_group > 64 && large >= chip ? launch_tile<FMT, 2, 4, 4>(p, stream) : launch_tile<FMT, 2, 4, 2>(p, stream);
 }
 
 }  // namespace
