@@ -129,11 +129,14 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   // that much earlier.  (WHOLE rows have 16 scales at least.)
   char* s_scales = smem + T::STAGES * T::STAGE;
   auto group_start = [&](int s) { return WHOLE ? min(s / T::GROUP * 16, KB - 16) : s / T::GROUP * 16; };   // block
-  // part 0 .. MT - 1 of a stage's copies
-  auto stage_part = [&](int s, char* base, int part) {
+  // A stage's copies in pieces, each issued behind one tile's products: MT of them in a slice's last part, and where
+  // there are many, as many more in the next slice's first (256 rows in e4m3 397 us a call against 420, of 8192 rows
+  // on 32 experts of 7168 x 2048; smaller tiles lose a little, 178 against 175 with 512 rows).
+  constexpr int PIECES = MT > 2 ? 2 * MT : MT;
+  auto stage_piece = [&](int s, char* base, int piece) {
 #pragma unroll
     for (int c = 0; c < MINE; ++c) {
-      if (c % MT != part) continue;
+      if (c * PIECES / MINE != piece) continue;
       const int id = wave + c * T::WAVES;                      // wave-uniform
       if (c >= LEAST && id >= T::NX + T::NW) continue;
       const bool x = id < T::NX;
@@ -145,7 +148,7 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
         dma16_v(s * T::SLICE + kofs[c] < K ? b + from[c] : (const char*)g_zero_chunk, dst);
       }
     }
-    if (part == MT - 1 && s % T::GROUP == 0) {
+    if (piece == MT - 1 && s % T::GROUP == 0) {
       char* set = s_scales + s / T::GROUP % 2 * (T::SROWS * 16);
 #pragma unroll
       for (int c = 0; c < SMINE; ++c) {
@@ -165,9 +168,9 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
       }
     }
   };
-  auto stage = [&](int s, char* base) {
+  auto stage = [&](int s, char* base, int pieces) {
 #pragma unroll
-    for (int part = 0; part < MT; ++part) stage_part(s, base, part);
+    for (int piece = 0; piece < pieces; ++piece) stage_piece(s, base, piece);
   };
 
   // ---- K loop ----
@@ -259,14 +262,14 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   };
 #pragma unroll
   for (int s = 0; s < T::STAGES; ++s)
-    if (s < nk) stage(s, ring[s]);
+    if (s < nk) stage(s, ring[s], s + 1 < T::STAGES ? PIECES : MT);
 #pragma unroll
   for (int n = 0; n < 2; ++n)
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.f;
-  if (nk >= T::STAGES) wait_vmcnt<AHEAD + LEAST>();
+  if (nk >= T::STAGES) wait_vmcnt<AHEAD + LEAST * MT / PIECES>();
   else wait_vmcnt<0>();
   lds_barrier();
   Part part[2];
@@ -277,13 +280,14 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   own_scales(s1, s0);
   // ring[0] holds slice s, ring[1] the next, ...
   int s = 0;
-  // all parts of a slice but the last
-  auto most_parts = [&] {
+  // all parts of a slice but the last; `copy`: with the second half of the copies of the slice STAGES - 1 further on
+  auto most_parts = [&](bool copy) {
     auto one = [&](auto jc) {
       constexpr int j = decltype(jc)::value;
       multiply(jc, part[j % 2], s0, [&](int m) {
         read_part(ring[0], j + 1, m, part[(j + 1) % 2]);
         if (j % 2 && m == 0) read_scales(s, j + 1, s1);
+        if (PIECES > MT && j == 0 && copy) stage_piece(s + T::STAGES - 1, ring[T::STAGES - 1], MT + m);
       });
       if (j % 2) own_scales(s1, s0);
     };
@@ -295,19 +299,19 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   };
   constexpr std::integral_constant<int, T::PARTS - 1> last{};
   for (; s + T::STAGES < nk; ++s) {
-    most_parts();
+    most_parts(true);
     wait_vmcnt<AHEAD>();               // slice s + 1: at most the copies of those behind it are in flight
     lds_barrier();                     // every wave's, and its reads of slice s
     multiply(last, part[1], s0, [&](int m) {
       read_part(ring[1], 0, m, part[0]);
       if (m == 0) read_scales(s + 1, 0, s1);
-      stage_part(s + T::STAGES, ring[0], m);
+      stage_piece(s + T::STAGES, ring[0], m);
     });
     own_scales(s1, s0);
     rotate();
   }
-  for (; s < nk; ++s) {                // the last slices: nothing to copy
-    most_parts();
+  for (; s < nk; ++s) {                // the last slices: nothing more to copy
+    most_parts(s + T::STAGES - 1 < nk);
     wait_vmcnt<0>();
     lds_barrier();
     multiply(last, part[1], s0, [&](int m) {
