@@ -36,13 +36,13 @@ __device__ __forceinline__ i32x8 narrow(u32x4 v) {
 }
 
 // a slice: KS values of K
-template <int FMT, int WM, int WN, int MT, int MOST_STAGES, int KS>
+template <int FMT, int WM, int WN, int MT, int NT, int MOST_STAGES, int KS>
 struct MxTile {
-  static constexpr int F = FMT, M_WAVES = WM, N_WAVES = WN, M_TILES = MT;
+  static constexpr int F = FMT, M_WAVES = WM, N_WAVES = WN, M_TILES = MT, N_TILES = NT;
   static constexpr int WAVES = WM * WN;
   static constexpr int NTH = WAVES * 64;
   static constexpr int BM = WM * MT * 32;
-  static constexpr int BN = WN * 64;                          // weight rows
+  static constexpr int BN = WN * NT * 32;                     // weight rows
   static constexpr int SLICE = KS, PARTS = KS / 64;           // (a part: what one instruction takes)
   static constexpr int XROW = FMT == MX_E4M3 ? KS : KS / 2;   // bytes of a slice's row
   static constexpr int WROW = KS / 2;
@@ -56,9 +56,10 @@ struct MxTile {
   static constexpr int STAGES = FIT < MOST_STAGES ? FIT : MOST_STAGES;
   static constexpr int LDS = STAGE * STAGES + 2 * SROWS * 16;
   static constexpr int NX = X_BYTES / 1024, NW = W_BYTES / 1024, NS = SROWS / 64;   // wave copies
-  // the same workgroup for a group's last rows, where fewer than BM are left
-  template <int FEWER>
-  using Low = MxTile<FMT, WM, WN, FEWER, MOST_STAGES, KS>;
+  // as many waves and weight rows for a group's last rows, where 64 ROWS64 will do
+  template <int ROWS64>
+  using Low = MxTile<FMT, 2, 4, ROWS64, 2, MOST_STAGES, KS>;
+  static constexpr int LOWS = WAVES == 8 && BN == 256 ? (BM - 1) / 128 + (BM > 64) : 0;
   static_assert(X_BYTES % 1024 == 0 && W_BYTES % 1024 == 0, "whole wave copies");
   static_assert(STAGES >= 2, "a slice on its way beside the one in use");
   static_assert(STAGES <= GROUP + 1, "the scales of slice s + STAGES replace those of two groups before");
@@ -76,7 +77,7 @@ __device__ __forceinline__ int mx_chunk(int row, int c) {
 // rows row0 .. row0 + rows of group g (1 <= rows <= BM), output features feat0 ..
 template <class T, bool SWIGLU, bool WHOLE>
 __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int g, int64_t row0, int rows, int feat0) {
-  constexpr int FMT = T::F, MT = T::M_TILES;
+  constexpr int FMT = T::F, MT = T::M_TILES, NT = T::N_TILES, STEPS = MT * NT / 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int K = p.K, N = p.N;
 
@@ -129,10 +130,10 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   // that much earlier.  (WHOLE rows have 16 scales at least.)
   char* s_scales = smem + T::STAGES * T::STAGE;
   auto group_start = [&](int s) { return WHOLE ? min(s / T::GROUP * 16, KB - 16) : s / T::GROUP * 16; };   // block
-  // A stage's copies in pieces, each issued behind one tile's products: MT of them in a slice's last part, and where
+  // A stage's copies in pieces, each issued behind two tiles' products: STEPS of them in a slice's last part, and where
   // there are many, as many more in the next slice's first (256 rows in e4m3 397 us a call against 420, of 8192 rows
   // on 32 experts of 7168 x 2048; smaller tiles lose a little, 178 against 175 with 512 rows).
-  constexpr int PIECES = MT > 2 ? 2 * MT : MT;
+  constexpr int PIECES = STEPS > 2 ? 2 * STEPS : STEPS;
   auto stage_piece = [&](int s, char* base, int piece) {
 #pragma unroll
     for (int c = 0; c < MINE; ++c) {
@@ -148,7 +149,7 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
         dma16_v(s * T::SLICE + kofs[c] < K ? b + from[c] : (const char*)g_zero_chunk, dst);
       }
     }
-    if (piece == MT - 1 && s % T::GROUP == 0) {
+    if (piece == STEPS - 1 && s % T::GROUP == 0) {
       char* set = s_scales + s / T::GROUP % 2 * (T::SROWS * 16);
 #pragma unroll
       for (int c = 0; c < SMINE; ++c) {
@@ -179,19 +180,18 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   constexpr int AHEAD = (T::STAGES - 2) * LEAST;
   const int wm = wave / T::N_WAVES, wn = wave % T::N_WAVES;
   const int r = lane & 31, q = lane >> 5;
-  f32x16 acc[2][MT];
+  f32x16 acc[NT][MT];
 
   struct Part {                        // operands of 64 values of K
-    i32x8 w[2], x[MT];
+    i32x8 w[NT], x[MT];
   };
   struct Scales {                      // of two parts: 4 blocks; shifted by the lane's q, bytes 0 and 2 are its own
-    int w[2], x[MT];
+    int w[NT], x[MT];
   };
-  const int wrow = wn * 64 + r, xrow = wm * MT * 32 + r;
-  auto read_w = [&](const char* base, int j, Part& h) {
+  const int wrow = wn * NT * 32 + r, xrow = wm * MT * 32 + r;
+  auto read_w = [&](const char* base, int j, int n, Part& h) {
     const char* W = base + T::X_BYTES + wrow * T::WROW + mx_chunk<T::WROW>(wrow, 2 * j + q) * 16;
-#pragma unroll
-    for (int n = 0; n < 2; ++n) h.w[n] = narrow(ld16(W + n * 32 * T::WROW));
+    h.w[n] = narrow(ld16(W + n * 32 * T::WROW));
   };
   auto read_x = [&](const char* base, int j, int m, Part& h) {
     if constexpr (FMT == MX_E4M3) {
@@ -207,14 +207,14 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   auto read_scales = [&](int i, int j, Scales& s) {              // of slice i, parts j and j + 1
     const char* S = s_scales + i / T::GROUP % 2 * (T::SROWS * 16) + (T::SLICE / 32 * i - group_start(i)) + 2 * j;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) s.w[n] = *reinterpret_cast<const int*>(S + (T::BM + wrow + n * 32) * 16);
+    for (int n = 0; n < NT; ++n) s.w[n] = *reinterpret_cast<const int*>(S + (T::BM + wrow + n * 32) * 16);
 #pragma unroll
     for (int m = 0; m < MT; ++m) s.x[m] = *reinterpret_cast<const int*>(S + (xrow + m * 32) * 16);
   };
   // (apart from the read: a shift beside it would wait for it, and for the operands read before it)
   auto own_scales = [&](const Scales& all, Scales& s) {
 #pragma unroll
-    for (int n = 0; n < 2; ++n) s.w[n] = (uint32_t)all.w[n] >> (8 * q);
+    for (int n = 0; n < NT; ++n) s.w[n] = (uint32_t)all.w[n] >> (8 * q);
 #pragma unroll
     for (int m = 0; m < MT; ++m) s.x[m] = (uint32_t)all.x[m] >> (8 * q);
   };
@@ -228,27 +228,26 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     constexpr int j = decltype(jc)::value;
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
+    for (int i = 0; i < STEPS; ++i) {
+      const int m = 2 * i / NT, n0 = 2 * i % NT;
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int n = n0; n < n0 + 2; ++n)
         acc[n][m] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(h.w[n], h.x[m], acc[n][m], 4, FMT == MX_E4M3 ? 0 : 4,
                                                                     2 * (j % 2), s.w[n], 2 * (j % 2), s.x[m]);
-      asm volatile("" : "+v"(acc[0][m]), "+v"(acc[1][m]));
+      asm volatile("" : "+v"(acc[n0][m]), "+v"(acc[n0 + 1][m]));
       __builtin_amdgcn_sched_barrier(0);
-      other(m);
+      other(i);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  // the next half's operands: the weights and the first tile's rows, then the other tiles'
-  auto read_part = [&](const char* base, int j, int m, Part& h) {
-    if (m == 0) {
-      read_w(base, j, h);
-      read_x(base, j, 0, h);
-    }
-    constexpr int EACH = MT > 2 ? (MT - 1 + MT - 3) / (MT - 2) : 1;
+  // the next part's operands, weights first, spread over all steps but the last
+  auto read_step = [&](const char* base, int j, int i, Part& h) {
 #pragma unroll
-    for (int t = 1; t < MT; ++t)
-      if ((MT > 2 ? 1 + (t - 1) / EACH : 0) == m) read_x(base, j, t, h);
+    for (int k = 0; k < NT + MT; ++k) {
+      if (k * (STEPS > 1 ? STEPS - 1 : 1) / (NT + MT) != i) continue;
+      if (k < NT) read_w(base, j, k, h);
+      else read_x(base, j, k - NT, h);
+    }
   };
 
   char* ring[T::STAGES];
@@ -262,20 +261,20 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   };
 #pragma unroll
   for (int s = 0; s < T::STAGES; ++s)
-    if (s < nk) stage(s, ring[s], s + 1 < T::STAGES ? PIECES : MT);
+    if (s < nk) stage(s, ring[s], s + 1 < T::STAGES ? PIECES : STEPS);
 #pragma unroll
-  for (int n = 0; n < 2; ++n)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[n][m][i] = 0.f;
-  if (nk >= T::STAGES) wait_vmcnt<AHEAD + LEAST * MT / PIECES>();
+  if (nk >= T::STAGES) wait_vmcnt<AHEAD + LEAST * STEPS / PIECES>();
   else wait_vmcnt<0>();
   lds_barrier();
   Part part[2];
   Scales s0, s1;
 #pragma unroll
-  for (int m = 0; m < MT; ++m) read_part(ring[0], 0, m, part[0]);
+  for (int i = 0; i < STEPS; ++i) read_step(ring[0], 0, i, part[0]);
   read_scales(0, 0, s1);
   own_scales(s1, s0);
   // ring[0] holds slice s, ring[1] the next, ...
@@ -284,10 +283,10 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   auto most_parts = [&](bool copy) {
     auto one = [&](auto jc) {
       constexpr int j = decltype(jc)::value;
-      multiply(jc, part[j % 2], s0, [&](int m) {
-        read_part(ring[0], j + 1, m, part[(j + 1) % 2]);
-        if (j % 2 && m == 0) read_scales(s, j + 1, s1);
-        if (PIECES > MT && j == 0 && copy) stage_piece(s + T::STAGES - 1, ring[T::STAGES - 1], MT + m);
+      multiply(jc, part[j % 2], s0, [&](int i) {
+        read_step(ring[0], j + 1, i, part[(j + 1) % 2]);
+        if (j % 2 && i == 0) read_scales(s, j + 1, s1);
+        if (PIECES > STEPS && j == 0 && copy) stage_piece(s + T::STAGES - 1, ring[T::STAGES - 1], STEPS + i);
       });
       if (j % 2) own_scales(s1, s0);
     };
@@ -302,10 +301,10 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     most_parts(true);
     wait_vmcnt<AHEAD>();               // slice s + 1: at most the copies of those behind it are in flight
     lds_barrier();                     // every wave's, and its reads of slice s
-    multiply(last, part[1], s0, [&](int m) {
-      read_part(ring[1], 0, m, part[0]);
-      if (m == 0) read_scales(s + 1, 0, s1);
-      stage_piece(s + T::STAGES, ring[0], m);
+    multiply(last, part[1], s0, [&](int i) {
+      read_step(ring[1], 0, i, part[0]);
+      if (i == 0) read_scales(s + 1, 0, s1);
+      stage_piece(s + T::STAGES, ring[0], i);
     });
     own_scales(s1, s0);
     rotate();
@@ -314,9 +313,9 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     most_parts(s + T::STAGES - 1 < nk);
     wait_vmcnt<0>();
     lds_barrier();
-    multiply(last, part[1], s0, [&](int m) {
-      read_part(ring[1], 0, m, part[0]);   // (behind the last slice: what lies there, not used)
-      if (m == 0) read_scales(min(s + 1, nk - 1), 0, s1);
+    multiply(last, part[1], s0, [&](int i) {
+      read_step(ring[1], 0, i, part[0]);   // (behind the last slice: what lies there, not used)
+      if (i == 0) read_scales(min(s + 1, nk - 1), 0, s1);
     });
     own_scales(s1, s0);
     rotate();
@@ -328,47 +327,50 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     const int local = (wm * MT + m) * 32 + r;
     const int64_t row = row0 + local;
     if constexpr (SWIGLU) {
-      const int f0 = feat0 + wn * 32;
-      float a[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float h = acc[0][m][i], u = acc[1][m][i];
-        a[i] = h * __builtin_amdgcn_rcpf(1.0f + __expf(-h)) * u;
-      }
-      uint32_t most = abs_max_bits(a);
-      most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
-      const uint32_t s = mx_scale_byte<FMT>(most);
-      const bool live = local < rows && f0 < N;               // N is whole blocks
-      if constexpr (FMT == MX_E4M3) {
-        // groups g of 4 features as dwords; lane q ends up with features 16 q .. 16 q + 15
-        uint32_t w[4];
+      for (int n = 0; n < NT; n += 2) {
+        const int f0 = feat0 + wn * NT * 16 + n * 16;
+        float a[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = mx_pack4_e4m3(a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3], s);
-        const uint32_t o0 = (uint32_t)__shfl_xor((int)(q ? w[0] : w[2]), 32, 64);
-        const uint32_t o1 = (uint32_t)__shfl_xor((int)(q ? w[1] : w[3]), 32, 64);
-        const u32x4 v = q ? u32x4{o0, w[2], o1, w[3]} : u32x4{w[0], o0, w[1], o1};
-        if (live) st16(p.Yq + row * N + f0 + 16 * q, v);
-      } else {
-        // pairs of groups: 4 half-bytes each, merged with the partner's
-        float lo[8], hi[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          lo[i] = a[i];
-          hi[i] = a[8 + i];
+        for (int i = 0; i < 16; ++i) {
+          const float h = acc[n][m][i], u = acc[n + 1][m][i];
+          a[i] = h * __builtin_amdgcn_rcpf(1.0f + __expf(-h)) * u;
         }
-        const uint32_t w0 = mx_pack8_e2m1(lo, s), w1 = mx_pack8_e2m1(hi, s);   // groups 0, 1 and 2, 3
-        const uint32_t o = (uint32_t)__shfl_xor((int)(q ? w0 : w1), 32, 64);
-        const uint32_t own = q ? w1 : w0;
-        // dword of 8 features = low half of lane q = 0's group, then lane q = 1's
-        const uint32_t e = q ? (o & 0xffffu) | (own << 16) : (own & 0xffffu) | (o << 16);
-        const uint32_t f = q ? (o >> 16) | (own & 0xffff0000u) : (own >> 16) | (o & 0xffff0000u);
-        if (live) *reinterpret_cast<u32x2*>(p.Yq + (row * N + f0) / 2 + 8 * q) = u32x2{e, f};
+        uint32_t most = abs_max_bits(a);
+        most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
+        const uint32_t s = mx_scale_byte<FMT>(most);
+        const bool live = local < rows && f0 < N;               // N is whole blocks
+        if constexpr (FMT == MX_E4M3) {
+          // groups g of 4 features as dwords; lane q ends up with features 16 q .. 16 q + 15
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = mx_pack4_e4m3(a[4 * i], a[4 * i + 1], a[4 * i + 2], a[4 * i + 3], s);
+          const uint32_t o0 = (uint32_t)__shfl_xor((int)(q ? w[0] : w[2]), 32, 64);
+          const uint32_t o1 = (uint32_t)__shfl_xor((int)(q ? w[1] : w[3]), 32, 64);
+          const u32x4 v = q ? u32x4{o0, w[2], o1, w[3]} : u32x4{w[0], o0, w[1], o1};
+          if (live) st16(p.Yq + row * N + f0 + 16 * q, v);
+        } else {
+          // pairs of groups: 4 half-bytes each, merged with the partner's
+          float lo[8], hi[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            lo[i] = a[i];
+            hi[i] = a[8 + i];
+          }
+          const uint32_t w0 = mx_pack8_e2m1(lo, s), w1 = mx_pack8_e2m1(hi, s);   // groups 0, 1 and 2, 3
+          const uint32_t o = (uint32_t)__shfl_xor((int)(q ? w0 : w1), 32, 64);
+          const uint32_t own = q ? w1 : w0;
+          // dword of 8 features = low half of lane q = 0's group, then lane q = 1's
+          const uint32_t e = q ? (o & 0xffffu) | (own << 16) : (own & 0xffffu) | (o << 16);
+          const uint32_t f = q ? (o >> 16) | (own & 0xffff0000u) : (own >> 16) | (o & 0xffff0000u);
+          if (live) *reinterpret_cast<u32x2*>(p.Yq + (row * N + f0) / 2 + 8 * q) = u32x2{e, f};
+        }
+        if (live && q == 0) p.Y_scales[row * (N / 32) + f0 / 32] = (uint8_t)s;
       }
-      if (live && q == 0) p.Y_scales[row * (N / 32) + f0 / 32] = (uint8_t)s;
     } else {
 #pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const int f0 = feat0 + wn * 64 + n * 32;
+      for (int n = 0; n < NT; ++n) {
+        const int f0 = feat0 + wn * NT * 32 + n * 32;
         uint32_t w[4][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -452,15 +454,10 @@ __global__ __launch_bounds__(T::NTH) void k_mx_gemm(MxGemmProblem p) {
   const int rows = min(T::BM, __builtin_amdgcn_readlane(k.rows, l) - m0);   // >= 1
   const int feat0 = local / mine * FEAT;
   // a group's last rows: as many of a wave's tiles as they need
-  constexpr int MT = T::M_TILES;
-  if constexpr (MT > 1) {
-    using Low = typename T::template Low<1>;
-    if (rows <= Low::BM) return mx_tile<Low, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
-  }
-  if constexpr (MT > 2) {
-    using Low = typename T::template Low<2>;
-    if (rows <= Low::BM) return mx_tile<Low, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
-  }
+  if constexpr (T::LOWS > 0)
+    if (rows <= 64) return mx_tile<typename T::template Low<1>, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
+  if constexpr (T::LOWS > 1)
+    if (rows <= 128) return mx_tile<typename T::template Low<2>, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
   mx_tile<T, SWIGLU, WHOLE>(p, smem, g, row0, rows, feat0);
 }
 
@@ -468,8 +465,8 @@ __global__ __launch_bounds__(T::NTH) void k_mx_gemm(MxGemmProblem p) {
 template <class T>
 constexpr int launch_lds() {
   int most = T::LDS;
-  if (T::M_TILES > 1 && T::template Low<1>::LDS > most) most = T::template Low<1>::LDS;
-  if (T::M_TILES > 2 && T::template Low<2>::LDS > most) most = T::template Low<2>::LDS;
+  if (T::LOWS > 0 && T::template Low<1>::LDS > most) most = T::template Low<1>::LDS;
+  if (T::LOWS > 1 && T::template Low<2>::LDS > most) most = T::template Low<2>::LDS;
   return most;
 }
 
@@ -495,16 +492,16 @@ hipError_t launch_as(const MxGemmProblem& p, hipStream_t stream) {
 // each, rows of 64 cost as many accesses for half the bytes (2048 rows on 8 experts of 4096 x 14336: 395 us a call
 // against 444; 8192 rows: 841 against 874).  e4m3 rows have 128 bytes in slices of 128, and LDS has no room for two
 // such stages of 256 rows.
-template <int FMT, int WM, int WN, int MT>
+template <int FMT, int WM, int WN, int MT, int NT>
 hipError_t launch_tile(const MxGemmProblem& p, hipStream_t stream) {
-  if constexpr (FMT == MX_E2M1 && WN == 4) {
+  if constexpr (FMT == MX_E2M1 && WN * NT == 8) {
     if (p.K % 256 == 0 && p.K >= 512) {
-      using T = MxTile<FMT, WM, WN, MT, 3, 256>;
+      using T = MxTile<FMT, WM, WN, MT, NT, 3, 256>;
       return p.swiglu ? launch_as<T, true, true>(p, stream) : launch_as<T, false, true>(p, stream);
     }
   }
   // whole: no slice has a row's end inside, and a row has the scales of a group
-  using T = MxTile<FMT, WM, WN, MT, 4, 128>;
+  using T = MxTile<FMT, WM, WN, MT, NT, 4, 128>;
   const bool whole = p.K % 128 == 0 && p.K >= 512;
   if (p.swiglu) return whole ? launch_as<T, true, true>(p, stream) : launch_as<T, true, false>(p, stream);
   return whole ? launch_as<T, false, true>(p, stream) : launch_as<T, false, false>(p, stream);
@@ -526,8 +523,8 @@ hipError_t launch_format(const MxGemmProblem& p, hipStream_t stream) {
   // (a group ends half a tile early in the mean)
   const int64_t narrow = p.groups * ((per_group + 64 + 127) / 128) * ((weight_rows + 127) / 128);
   const int64_t large = p.groups * ((per_group + 255) / 256) * ((weight_rows + 255) / 256);
-  if (narrow <= chip) return launch_tile<FMT, 4, 2, 1>(p, stream);
-  return per_group > 64 && large >= chip ? launch_tile<FMT, 2, 4, 4>(p, stream) : launch_tile<FMT, 2, 4, 2>(p, stream);
+  if (narrow <= chip) return launch_tile<FMT, 4, 2, 1, 2>(p, stream);
+  return per_group > 64 && large >= chip ? launch_tile<FMT, 4, 2, 2, 4>(p, stream) : launch_tile<FMT, 2, 4, 2, 2>(p, stream);
 }
 
 }  // namespace
