@@ -388,32 +388,72 @@ constexpr int kBlockRow = 16384;    // longest row of a workgroup's registers (8
 
 }  // namespace
 
+// A launch has less than 2^32 threads; what needs more goes in parts of this many workgroups.
+constexpr int64_t kMostBlocks = int64_t(1) << 23;
+
+namespace {
+template <class T>
+T* rows_on(T* p, int64_t values) {
+  return p ? p + values : p;
+}
+template <class Launch>
+hipError_t convert_parts(MxConvertProblem p, Launch&& launch) {
+  const int64_t per = (int64_t)kThreads * kUnroll * 8, most = kMostBlocks * per;
+  for (int64_t left = p.n; left > 0; left -= most) {
+    p.n = left < most ? left : most;
+    launch(p, dim3((unsigned)((p.n + per - 1) / per)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    p.x = rows_on(p.x, most);
+    p.out = rows_on(p.out, most);
+    p.elements += p.format == MX_E2M1 ? most / 2 : most;
+    p.scales += most / 32;
+  }
+  return hipSuccess;
+}
+}  // namespace
+
 hipError_t launch_mx_quantize(const MxConvertProblem& p, hipStream_t stream) {
-  const int64_t per = (int64_t)kThreads * kUnroll * 8;
-  const unsigned blocks = (unsigned)((p.n + per - 1) / per);
-  if (p.format == MX_E2M1)
-    hipLaunchKernelGGL(k_mx_quantize<MX_E2M1>, dim3(blocks), dim3(kThreads), 0, stream, p);
-  else
-    hipLaunchKernelGGL(k_mx_quantize<MX_E4M3>, dim3(blocks), dim3(kThreads), 0, stream, p);
-  return hipGetLastError();
+  return convert_parts(p, [&](const MxConvertProblem& q, dim3 blocks) {
+    if (q.format == MX_E2M1)
+      hipLaunchKernelGGL(k_mx_quantize<MX_E2M1>, blocks, dim3(kThreads), 0, stream, q);
+    else
+      hipLaunchKernelGGL(k_mx_quantize<MX_E4M3>, blocks, dim3(kThreads), 0, stream, q);
+  });
 }
 
 hipError_t launch_mx_dequantize(const MxConvertProblem& p, hipStream_t stream) {
-  const int64_t per = (int64_t)kThreads * kUnroll * 8;
-  const unsigned blocks = (unsigned)((p.n + per - 1) / per);
-  if (p.format == MX_E2M1)
-    hipLaunchKernelGGL(k_mx_dequantize<MX_E2M1>, dim3(blocks), dim3(kThreads), 0, stream, p);
-  else
-    hipLaunchKernelGGL(k_mx_dequantize<MX_E4M3>, dim3(blocks), dim3(kThreads), 0, stream, p);
-  return hipGetLastError();
+  return convert_parts(p, [&](const MxConvertProblem& q, dim3 blocks) {
+    if (q.format == MX_E2M1)
+      hipLaunchKernelGGL(k_mx_dequantize<MX_E2M1>, blocks, dim3(kThreads), 0, stream, q);
+    else
+      hipLaunchKernelGGL(k_mx_dequantize<MX_E4M3>, blocks, dim3(kThreads), 0, stream, q);
+  });
 }
 
 namespace {
+// rows_per_block rows per workgroup
+template <class Kernel>
+hipError_t norm_parts(Kernel kernel, int rows_per_block, AddNormProblem p, hipStream_t stream) {
+  const int64_t most = kMostBlocks * rows_per_block;
+  for (int64_t left = p.rows; left > 0; left -= most) {
+    p.rows = left < most ? left : most;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((p.rows + rows_per_block - 1) / rows_per_block)), dim3(kThreads), 0, stream, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    p.x += most * p.d;
+    p.residual = rows_on(p.residual, most * p.d);
+    p.h = rows_on(p.h, most * p.d);
+    p.y = rows_on(p.y, most * p.d);
+    p.y_q = rows_on(p.y_q, most * p.d);
+    p.y_scales = rows_on(p.y_scales, most * (p.d / 32));
+    p.rstd = rows_on(p.rstd, most);
+  }
+  return hipSuccess;
+}
 template <int TPR, int VPT>
 hipError_t norm_as(const AddNormProblem& p, hipStream_t stream) {
-  constexpr int RPB = kThreads / TPR;
-  hipLaunchKernelGGL((k_add_norm<TPR, VPT>), dim3((unsigned)((p.rows + RPB - 1) / RPB)), dim3(kThreads), 0, stream, p);
-  return hipGetLastError();
+  return norm_parts(k_add_norm<TPR, VPT>, kThreads / TPR, p, stream);
 }
 template <int TPR, int VPT>
 hipError_t norm_bwd_as(const AddNormBwdProblem& p, int parts, hipStream_t stream) {
@@ -432,8 +472,7 @@ hipError_t launch_add_norm(const AddNormProblem& p, hipStream_t stream) {
   if (p.d <= 4096) return norm_as<256, 2>(p, stream);
   if (p.d <= 8192) return norm_as<256, 4>(p, stream);
   if (p.d <= kBlockRow) return norm_as<256, 8>(p, stream);
-  hipLaunchKernelGGL(k_add_norm_long, dim3((unsigned)p.rows), dim3(kThreads), 0, stream, p);
-  return hipGetLastError();
+  return norm_parts(k_add_norm_long, 1, p, stream);
 }
 
 hipError_t launch_add_norm_bwd(const AddNormBwdProblem& p, hipStream_t stream) {

@@ -101,6 +101,25 @@ def test_forward_options(d):
     run_forward(5, d, residual=False, q=True)
 
 
+def test_more_rows_than_a_launch_has_threads_for():
+    """2^28 + 3 rows of 8 values: offsets past 32 bits, and eight launches and a rest; every row against the formula in
+    float64, in pieces."""
+    rows, d, eps = (1 << 28) + 3, 8, 1e-5
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x, y = torch.empty((rows, d), dtype=BF16, device="cuda"), torch.full((rows + 1, d), -3.0, dtype=BF16, device="cuda")
+    for a in range(0, rows, 1 << 24):
+        x[a:a + (1 << 24)].normal_(generator=g)
+    gamma = torch.randn(d, generator=torch.Generator().manual_seed(5)).to(BF16).cuda()
+    moe.moe_add_rmsnorm(x, None, gamma, eps, None, y[:rows])
+    for a in range(0, rows, 1 << 24):
+        b = min(rows, a + (1 << 24))
+        h = x[a:b].double()
+        ref = h / (h.pow(2).mean(1, keepdim=True) + eps).sqrt() * gamma.double()
+        # half a step of bf16 and the statistics' float32 error
+        assert ((y[a:b].double() - ref).abs() <= (2.0 ** -8 + 2.0 ** -18) * ref.abs()).all(), a
+    assert (y[rows] == -3.0).all()
+
+
 def test_forward_scales_and_eps():
     for std in (1e-18, 1e-4, 1e4, 1e15):
         run_forward(4, 1088, std=std, eps=0.0)

@@ -97,6 +97,23 @@ def test_dequantize_undoes_quantize(fmt):
         assert torch.equal(again, buf[:rows])
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_offsets_past_32_bits(fmt):
+    """2^31 values and some rows: the last rows as alone, and back."""
+    cols = 1024
+    rows = (1 << 31) // cols + 5
+    x = torch.zeros((rows, cols), dtype=torch.bfloat16, device="cuda")
+    x[-9:].normal_(generator=torch.Generator(device="cuda").manual_seed(2))
+    q, s = torch.empty((rows, moe.mx_elements_per_row(fmt, cols)), dtype=U8, device="cuda"), torch.empty((rows, cols // 32), dtype=U8, device="cuda")
+    moe.moe_mx_quantize(fmt, x, q, s)
+    codes, scales = mx.quantize(x[-9:].double().cpu().numpy(), fmt)
+    np.testing.assert_array_equal(s[-9:].cpu().numpy(), scales)
+    np.testing.assert_array_equal(q[-9:].cpu().numpy(), mx.pack(codes, fmt))
+    assert not q[:-9].any() and not s[:-9].any()
+    moe.moe_mx_dequantize(fmt, q, s, x)
+    np.testing.assert_array_equal(x[-9:].double().cpu().numpy(), mx.values(codes, scales, fmt))
+
+
 # ---- expert MLP ----
 def weights(rng, rows, K):
     """e2m1 weights of fan-in K: (elements, scales) on the GPU and their float64 values."""
@@ -218,6 +235,28 @@ def test_mlp_long_sums_keep_float32(fmt):
                            dev(mx.pack(wc, mx.E2M1)), dev(wsc), w2, s2, y, moe.alloc_workspace(sh, moe.MOE_WS_MX_FFN))
     ref = mlp64(mx.values(xc, xs, fmt), mx.values(wc, wsc, mx.E2M1), v2, fmt)
     assert np.linalg.norm(y.double().cpu().numpy() - ref) <= REL * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_mlp_offsets_past_32_bits(fmt):
+    """Rows whose elements and results lie past 2^31 (values of the result, bytes of 8-bit rows): the last expert's 9
+    rows against float64, the others' zeros."""
+    d, F, before, n = 7168, 32, 300003, 9
+    rows = before + n
+    sh = MoEShape(T=rows, d=d, E=2, top_k=1, F=F, E_local=2)
+    rng = np.random.default_rng(6)
+    codes, scales = mx.quantize(mx.bf16_values(f32_to_bf16_bits(rng.standard_normal((n, d)).astype(np.float32))), fmt)
+    q = torch.zeros((rows, moe.mx_elements_per_row(fmt, d)), dtype=U8, device="cuda")
+    s = torch.full((rows, d // 32), 127, dtype=U8, device="cuda")
+    q[before:], s[before:] = dev(mx.pack(codes, fmt)), dev(scales)
+    w13, s13, v13 = weights(rng, 2 * 2 * F, d)
+    w2, s2, v2 = weights(rng, 2 * d, F)
+    y = torch.full((rows, d), -77.0, dtype=torch.bfloat16, device="cuda")
+    moe.moe_mx_grouped_ffn(sh, fmt, q, s, dev(np.array([0, before, rows], np.int32)), w13, s13, w2, s2, y,
+                           moe.alloc_workspace(sh, moe.MOE_WS_MX_FFN))
+    assert not y[:before].any()
+    ref = mlp64(mx.values(codes, scales, fmt), v13[2 * F:], v2[d:], fmt)
+    assert np.linalg.norm(y[before:].double().cpu().numpy() - ref) <= REL * np.linalg.norm(ref)
 
 
 def test_mlp_replays_in_a_graph():

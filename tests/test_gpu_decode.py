@@ -160,6 +160,41 @@ def test_matches_the_layer():
 
 
 @pytest.mark.parametrize("mixed", [False, True])
+def test_weight_offsets_past_32_bits(mixed):
+    """160 experts of 2048 x 7168: the last ones' weights lie past 2^31 values and, in bf16, past 2^32; a router bias
+    sends every token to the last four."""
+    T, d, F, E = 3, 7168, 2048, 160
+    sh = MoEShape(T=T, d=d, E=E, top_k=4, F=F, E_local=E)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    x = torch.empty((T, d), device="cuda").normal_(generator=g).to(torch.bfloat16)
+    router = (torch.empty((E, d), device="cuda").normal_(generator=g) * d ** -0.5).to(torch.bfloat16)
+    bias = torch.zeros(E, device="cuda")
+    bias[-4:] = 100.0
+    kept = {}
+    w = {}
+    for name, rows, K in (("w13", 2 * F, d), ("w2", d, F)):
+        last = (torch.empty((4 * rows, K), device="cuda").normal_(generator=g) * K ** -0.5).to(torch.bfloat16)
+        if mixed:
+            q, s = (torch.empty((E * rows, n), dtype=torch.uint8, device="cuda") for n in (K // 2, K // 32))
+            q.fill_(0x77), s.fill_(254)                        # what other experts hold would be seen
+            moe.moe_mx_quantize(mx.E2M1, last, q[-4 * rows:], s[-4 * rows:])
+            moe.moe_mx_dequantize(mx.E2M1, q[-4 * rows:], s[-4 * rows:], last)
+            w[name] = (q, s)
+        else:
+            w[name] = (torch.full((E * rows, K), float("nan"), dtype=torch.bfloat16, device="cuda"), None)
+            w[name][0][-4 * rows:] = last
+        kept[name] = last.double().cpu().numpy().reshape(4, rows, K)
+    out, ws = torch.empty_like(x), moe.alloc_workspace(sh, moe.MOE_WS_DECODE)
+    moe.moe_layer_decode(sh, x, router, bias, w["w13"][0], w["w2"][0], None, None, out, ws,
+                         (w["w13"][1], w["w2"][1], None, None) if mixed else None)
+    xv, L = x.double().cpu().numpy(), x.double().cpu().numpy() @ router.double().cpu().numpy().T + bias.double().cpu().numpy()
+    gates = np.exp(L[:, -4:] - L.max(1, keepdims=True))
+    gates /= gates.sum(1, keepdims=True)
+    ref = sum(gates[:, i:i + 1] * oracle.swiglu_ffn(xv, kept["w13"][i], kept["w2"][i]) for i in range(4))
+    assert pu.rel_fro(out.double().cpu().numpy(), ref) <= pu.REL_TOL
+
+
+@pytest.mark.parametrize("mixed", [False, True])
 def test_repeats_bit_for_bit_and_in_a_used_workspace(mixed):
     layer, first = check(SMALL.replace(T=40, F_shared=64), mixed)
     for fill in (0, 255, 0x7f):
