@@ -2,17 +2,26 @@
 // e2m1, on v_mfma_scale_f32_32x32x64_f8f6f4 (elements multiplied as they are, each block of 32 products
 // times both blocks' powers of two, float32 accumulation).
 //
-// A workgroup owns BM rows of one group and BN weight rows; its K loop runs over slices of 128 values in
-// a ring of LDS stages, filled by direct-to-LDS copies.  Each wave multiplies MT x 2 tiles of 32 x 32: the
-// weights are the first operand, so that a lane holds 16 of the 32 output features of one row, its partner
-// lane (l ^ 32) the others.
+// A workgroup owns BM rows of one group and BN weight rows; its K loop runs over slices of 128 or 256
+// values in a ring of LDS stages, filled by direct-to-LDS copies.  Each wave multiplies MT x NT tiles of
+// 32 x 32: the weights are the first operand, so that a lane holds 16 of the 32 output features of one
+// row, its partner lane (l ^ 32) the others.  A group's last rows run on a tile of 64 or 128 rows.
 //
-// The matrix cores are not to wait for LDS: a slice is multiplied in two halves of 64 values, each half's
-// operands being read from LDS while the half before it is multiplied.  The one barrier of a slice stands
-// between its halves.  There the whole slice is in registers, so its stage is free and takes the copies of
-// the slice STAGES further on; STAGES - 1 slices are on their way or landed.
+// The matrix cores are not to wait for LDS: a slice is multiplied in parts of 64 values, each part's
+// operands being read from LDS between the products of the part before it.  The one barrier of a slice
+// stands before its last part.  There the whole slice is in registers, so its stage is free and takes the
+// copies of the slice STAGES further on; STAGES - 1 slices are on their way or landed.
 //
-// SwiGLU: a wave's two weight tiles are the gate and the up rows of the same 32 features, so the
+// What bounds it: with many rows the matrix cores' power.  Bare loops of the instruction on random
+// operands run at 3.4 - 4.0 PFLOP/s (e4m3 rows) and 6.2 - 6.6 (e2m1), a fifth to a third below those on
+// zeros, and the clock in these kernels is 1.9 GHz; the rest is the share of LDS and L2 in that power and
+// the 5 us in which a tile begins and ends.  8192 rows on 8 experts of 4096 x 14336 in e2m1: 0.95 ms a
+// call, 3.1 PFLOP/s (0.83 ms with loads that are whole tiles; its products alone 0.44); 8192 on 32 of
+// 7168 x 2048 in e4m3: 0.45 ms (0.39; 0.21).  Of even loads of the latter, 416 us then: without the
+// products 344, without the copies 330, without LDS reads and copies 292.  With few rows it is the
+// weights' stream: 512 rows on the 32 experts 0.18 ms, 4.1 TB/s; 501 rows on 8 of 2048 x 1408 24 us.
+//
+// SwiGLU: two weight tiles of a wave are the gate and the up rows of the same 32 features, so the
 // activation and the maximum of its block are formed in registers, and the block leaves as elements and
 // one scale.
 //
@@ -218,10 +227,10 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
 #pragma unroll
     for (int m = 0; m < MT; ++m) s.x[m] = (uint32_t)all.x[m] >> (8 * q);
   };
-  // One half's products (16 per wave and more than twice as many cycles of the matrix core as LDS needs for the next
-  // half's operands), with the wave's other work between them: an instruction waits for those before it, so reads or
-  // copies in one piece would leave the matrix core idle until the last of all eight waves' had been issued.  `other(m)`
-  // is issued behind the products of tile m, all reads before the last tile's.
+  // One part's products, with the wave's other work between them: an instruction waits for those before it, so reads or
+  // copies in one piece would leave the matrix core idle until the last of all eight waves' had been issued (930 us a
+  // call against 887, of 1024 rows on each of 8 experts of 4096 x 14336 in e2m1).  `other(i)` is issued behind the two
+  // products of step i, all reads before the last step's.
   // (Matrix instructions are no memory accesses to the compiler, which would move them all behind the barrier.  The empty
   // statement that claims to change their results keeps them where they stand.)
   auto multiply = [&](auto jc, const Part& h, const Scales& s, auto other) {

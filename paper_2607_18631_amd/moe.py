@@ -294,7 +294,8 @@ def moe_mx_dequantize(format, elements, scales, x, stream=None):
 
 
 def moe_mx_grouped_ffn(sh, format, x_q, x_scales, offsets, w13_q, w13_scales, w2_q, w2_scales, y_perm, ws, stream=None):
-    """``x_q`` / ``x_scales`` and ``y_perm`` have ``sh.capacity`` rows."""
+    """The expert MLP on block-scaled rows in expert order (``format``) and e2m1 weights.  ``x_q`` / ``x_scales`` and
+    ``y_perm`` have ``sh.capacity`` rows; ``offsets`` is ``moe_permute``'s, or with an expert capacity its counts."""
     d, F, El, cap = sh.d, sh.F, sh.E_local, sh.capacity
     dev = _matrix("y_perm", y_perm)[2]
     _on(dev, stream, _lib.moe_mx_grouped_ffn, ctypes.byref(shape_c(sh)), format,
@@ -306,6 +307,8 @@ def moe_mx_grouped_ffn(sh, format, x_q, x_scales, offsets, w13_q, w13_scales, w2
 
 
 def moe_add_rmsnorm(x, residual, gamma, eps, h, y, y_q=None, y_scales=None, rstd=None, stream=None):
+    """``h = x + residual``, ``y = h * rstd * gamma`` in bf16, in e4m3 blocks (``y_q``, ``y_scales``), or in both.
+    Without a residual ``h`` is None; with one it may be the buffer of ``x`` or of ``residual``."""
     rows, d, dev = _matrix("x", x)
     _on(dev, stream, _lib.moe_add_rmsnorm, rows, d, eps, _take(dev, "x", x, _bf16, rows, d),
         None if residual is None else _take(dev, "residual", residual, _bf16, rows, d), _take(dev, "gamma", gamma, _bf16, d),
@@ -316,6 +319,8 @@ def moe_add_rmsnorm(x, residual, gamma, eps, h, y, y_q=None, y_scales=None, rstd
 
 
 def moe_add_rmsnorm_backward(dy, dh, h, gamma, rstd, dx, dgamma, ws, stream=None):
+    """``dx`` (of x and of the residual alike) and ``dgamma``; ``dh`` is the gradient that comes back to ``h``, or None.
+    ``h`` and ``rstd`` are the forward's (``h`` is ``x`` where it had no residual)."""
     rows, d, dev = _matrix("dy", dy)
     _on(dev, stream, _lib.moe_add_rmsnorm_backward, rows, d, _take(dev, "dy", dy, _bf16, rows, d),
         None if dh is None else _take(dev, "dh", dh, _bf16, rows, d), _take(dev, "h", h, _bf16, rows, d),
@@ -336,8 +341,8 @@ def alloc_add_rmsnorm_workspace(rows: int, d: int, device="cuda"):
 
 
 def moe_layer_decode(sh, x, w_router, bias, w13, w2, ws13, ws2, out, ws, scales=None, stream=None):
-    """``scales``: None with bf16 weights, or (w13_scales, w2_scales, ws13_scales, ws2_scales) with e2m1 ones
-    (the last two None without a shared expert)."""
+    """The whole layer for ``sh.T <= MOE_DECODE_MAX_TOKENS`` tokens.  ``scales``: None with bf16 weights, or
+    (w13_scales, w2_scales, ws13_scales, ws2_scales) with e2m1 ones (the last two None without a shared expert)."""
     T, d, F, Fs, El = sh.T, sh.d, sh.F, sh.F_shared, sh.E_local
     dev = _matrix("x", x)[2]
     s = scales if scales is not None else (None,) * 4
