@@ -1,12 +1,36 @@
 """Code generation of the block-scaled grouped product and the few-token layer (CPU only): nothing is spilled, the
 direct-to-LDS copies keep their wait state behind M0, a stage's copies stand between matrix instructions, and the
 few-token layer never waits for all its loads inside its weight loop."""
+import os
 import re
+import shutil
+import subprocess
 from concurrent.futures import ThreadPoolExecutor
 
 import pytest
 
-from test_gemm_codegen import _device_asm, _mfma_loops, pytestmark  # noqa: F401
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_18631_amd", "csrc")
+HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+
+pytestmark = pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not available")
+
+
+def _device_asm(src, out):
+    from paper_2607_18631_amd import build
+    subprocess.run([HIPCC, *build.FLAGS, "-I", CSRC, "-x", "hip", "--cuda-device-only", "-S", os.path.join(CSRC, src), "-o", out],
+                   check=True, capture_output=True, text=True)
+    with open(out) as f:
+        return f.read()
+
+
+def _mfma_loops(lines):
+    """(first, last) lines of the innermost loops (a branch back to a label) with matrix instructions in them."""
+    label = {m.group(1): i for i, l in enumerate(lines) if (m := re.match(r"(\.LBB\d+_\d+):", l))}
+    back = [re.search(r"s_(?:cbranch_\w+|branch)\s+(\.LBB\d+_\d+)", l) for l in lines]
+    loops = [(label[m.group(1)], i) for i, m in enumerate(back) if m and label.get(m.group(1), i) < i]
+    loops = [(a, b) for a, b in loops if any(l.startswith("v_mfma") for l in lines[a:b])]
+    return [(a, b) for a, b in loops if not any((c, d) != (a, b) and a <= c and d <= b for c, d in loops)]
+
 
 SOURCES = ["mx_gemm.hip", "decode.hip"]
 
