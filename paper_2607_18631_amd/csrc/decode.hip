@@ -26,9 +26,9 @@
 //
 // Measured: 4 tokens on 8 experts of 4096 x 14336 in 4 bits, top-2, of which 5 to 7 are chosen: 101 - 119 us a call,
 // some 5 TB/s of weights; 64 tokens on 48 of 384 experts of 7168 x 2048 in 4 bits, top-8, and a shared expert: 210 us,
-// 4.1 TB/s (up 104 - 111 us, down 77 - 82, gate 15, logits 9.5, combine 4.5); one token, 128 experts of 2048 x 768 in
+// 4.1 TB/s (up 104 - 111 us, down 77 - 82, gate 13, logits 9.5, combine 4.5); one token, 128 experts of 2048 x 768 in
 // bf16, top-8: 37 us, of which the weights' stream is 16 at the rate of a copy and the five launches that wait for each other the
-// rest (up 14, down 7, gate 6, logits and combine 4 each).
+// rest (up 15, down 7, gate 5, logits and combine 4 each).
 #include <algorithm>
 #include <cmath>
 
@@ -173,22 +173,26 @@ __global__ __launch_bounds__(256) void k_decode_gate(DecodeProblem p) {
   __shared__ uint32_t s_kept[kDecodeTokens];
   const int tid = threadIdx.x, n = p.T * p.top_k, wave = tid >> 6;
   const int64_t t = (int64_t)blockIdx.x * 4 + wave;
+  if (tid < kDecodeTokens) s_kept[tid] = 0;
+  for (int e = tid; e < p.E_local; e += 256) s_mask[e] = 0ull;
   if (t < p.T) gate_token<PL>(p.gate, t, s_key[wave], s_gscore[wave]);
+  // (with other workgroups:) the choices reach the device's memory before the count does, and are read back behind it
+  if (gridDim.x > 1) __threadfence();
+  __syncthreads();
   if (gridDim.x > 1) {
-    // the choices reach the device's memory before the count does, and are read back behind it
-    __threadfence();
-    __syncthreads();
     if (tid == 0) s_last = atomicAdd(&p.plan->arrived, 1) == (int)gridDim.x - 1;
     __syncthreads();
     if (!s_last) return;
     __threadfence();
   }
-  if (tid < kDecodeTokens) s_kept[tid] = 0;
-  for (int e = tid; e < p.E_local; e += 256) s_mask[e] = 0ull;
-  __syncthreads();
-  for (int i = tid; i < n; i += 256) {
-    const int e = p.gate.topk_idx[i] - p.e_begin;
-    if (e >= 0 && e < p.E_local) atomicOr(&s_mask[e], 1ull << (i / p.top_k));
+  // this thread's slots and their local experts (-1: none)
+  constexpr int SLOTS = kDecodeSlots / 256;
+  int mine[SLOTS];
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j) {
+    const int i = tid + 256 * j, e = i < n ? p.gate.topk_idx[i] - p.e_begin : -1;
+    mine[j] = e < p.E_local ? e : -1;
+    if (mine[j] >= 0) atomicOr(&s_mask[e], 1ull << (i / p.top_k));
   }
   __syncthreads();
   const int cap = p.expert_capacity > 0 ? p.expert_capacity : kDecodeTokens;
@@ -218,9 +222,10 @@ __global__ __launch_bounds__(256) void k_decode_gate(DecodeProblem p) {
   const int most = decode_entries(p.T, p.top_k, p.E_local);
   for (int a = (total >> 16) + tid; a < most; a += 256) p.plan->entry[a].count = 0;
   __syncthreads();
-  for (int i = tid; i < n; i += 256) {
-    const int e = p.gate.topk_idx[i] - p.e_begin;
-    if (e >= 0 && e < p.E_local) {
+#pragma unroll
+  for (int j = 0; j < SLOTS; ++j) {
+    const int i = tid + 256 * j, e = mine[j];
+    if (e >= 0) {
       const int rank = __popcll(s_mask[e] & ((1ull << (i / p.top_k)) - 1));
       if (rank < cap) {
         p.plan->slot[(s_begin[e] & 0xffff) + rank] = i;
