@@ -449,6 +449,8 @@ class DeviceLayer:
         names = ("w13", "w2", "ws13", "ws2")
         w, scales = [getattr(self, n) for n in names], None
         if mx:
+            if getattr(self, "mx", None) is None:
+                _refuse("the layer has no e2m1 weights yet: quantize() makes them")
             w, scales = zip(*(self.mx.get(n, (None, None)) for n in names))
         moe_layer_decode(self.shape, self.x, self.w_router, self.bias, *w, self.out, self.ws_decode, scales, stream)
         return self.out

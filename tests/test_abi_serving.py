@@ -331,3 +331,10 @@ def test_host_layer_under_asan_ubsan(tmp_path):
                UBSAN_OPTIONS="print_stacktrace=1:halt_on_error=1")
     r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=120)
     assert r.returncode == 0 and r.stdout.strip().endswith("ALL OK"), r.stdout[-3000:] + r.stderr[-3000:]
+
+
+def test_decode_on_4_bit_weights_that_were_not_made():
+    layer = moe.DeviceLayer.__new__(moe.DeviceLayer)
+    layer.shape, layer.w13, layer.w2, layer.ws13, layer.ws2, layer.ws_decode = BASE, None, None, None, None, object()
+    with pytest.raises(moe.MoEError, match="quantize"):
+        layer.decode(mx=True)

@@ -101,6 +101,31 @@ def test_forward_options(d):
     run_forward(5, d, residual=False, q=True)
 
 
+@pytest.mark.parametrize("d", [64, 2048, 7168, 16416])
+def test_rows_of_no_finite_values_stay_alone(d):
+    """Forward and backward: a NaN or an infinity reaches its own row's results and, backward, dgamma."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    x, r, dy = (torch.empty((9, d), device="cuda").normal_(generator=g).to(BF16) for _ in range(3))
+    gamma = torch.ones(d, dtype=BF16, device="cuda")
+
+    def run():
+        h, y, dx, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x), torch.empty(9, device="cuda")
+        q, s = torch.empty((9, d), dtype=torch.uint8, device="cuda"), torch.empty((9, d // 32), dtype=torch.uint8, device="cuda")
+        dg = torch.empty_like(gamma)
+        moe.moe_add_rmsnorm(x, r, gamma, 1e-6, h, y, q, s, rstd)
+        moe.moe_add_rmsnorm_backward(dy, None, h, gamma, rstd, dx, dg, moe.alloc_add_rmsnorm_workspace(9, d))
+        return y, q, s, rstd, dx
+
+    good = run()
+    x[2, d - 1], x[6, 0] = float("nan"), float("inf")
+    got = run()
+    others = torch.tensor([0, 1, 3, 4, 5, 7, 8], device="cuda")
+    assert all(torch.equal(a[others], b[others]) for a, b in zip(got, good))
+    assert torch.isnan(got[0][2]).all() and (got[2][2] == 255).all() and torch.isnan(got[4][2]).all()
+    # an infinite row: rstd is 0, so its finite values give 0 and the infinite one NaN
+    assert got[3][6] == 0 and (got[0][6, 1:] == 0).all() and torch.isnan(got[0][6, 0])
+
+
 def test_more_rows_than_a_launch_has_threads_for():
     """2^28 + 3 rows of 8 values: offsets past 32 bits, and eight launches and a rest; every row against the formula in
     float64, in pieces."""

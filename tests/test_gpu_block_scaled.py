@@ -259,6 +259,39 @@ def test_mlp_offsets_past_32_bits(fmt):
     assert np.linalg.norm(y[before:].double().cpu().numpy() - ref) <= REL * np.linalg.norm(ref)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_mlp_rows_of_no_finite_values_stay_alone(fmt):
+    """Rows that hold a NaN, an infinity, or e4m3's NaN code under a finite scale; and bf16's largest values, whose
+    activation overflows: the other rows' results do not change by a bit."""
+    d, F, n = 512, 96, 70
+    sh = MoEShape(T=n, d=d, E=2, top_k=1, F=F, E_local=2)
+    rng = np.random.default_rng(14)
+    w13, s13, _ = weights(rng, 2 * 2 * F, d)
+    w2, s2, _ = weights(rng, 2 * d, F)
+    off = dev(np.array([0, 33, n], np.int32))
+    x = moe.to_device_bf16(f32_to_bf16_bits(rng.standard_normal((n, d)).astype(np.float32)))
+    ws = moe.alloc_workspace(sh, moe.MOE_WS_MX_FFN)
+
+    def run(code=False):
+        q, s = torch.empty((n, moe.mx_elements_per_row(fmt, d)), dtype=U8, device="cuda"), torch.empty((n, d // 32), dtype=U8, device="cuda")
+        moe.moe_mx_quantize(fmt, x, q, s)
+        if code:
+            q[40, 17] = 0x7f
+        y = torch.empty((n, d), dtype=torch.bfloat16, device="cuda")
+        moe.moe_mx_grouped_ffn(sh, fmt, q, s, off, w13, s13, w2, s2, y, ws)
+        return y
+
+    good = run()
+    x[0, 5], x[31, 511], x[69] = float("nan"), float("inf"), 3.0e38
+    bad = [0, 31, 69] + ([40] if fmt == mx.E4M3 else [])
+    got = run(code=fmt == mx.E4M3)
+    others = torch.ones(n, dtype=torch.bool, device="cuda")
+    others[bad] = False
+    assert torch.equal(got[others], good[others])
+    for r in bad:
+        assert not torch.isfinite(got[r]).any(), r
+
+
 def test_mlp_replays_in_a_graph():
     """Captured conversion and MLP, replayed on new rows with eager work in between."""
     d, F, E = 256, 192, 4

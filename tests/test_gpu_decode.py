@@ -159,6 +159,24 @@ def test_matches_the_layer():
     assert pu.rel_fro(b, a) <= 2 * pu.REL_TOL
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), 3.0e38])
+@pytest.mark.parametrize("mixed", [False, True])
+def test_a_token_of_no_finite_values_stays_alone(bad, mixed):
+    """Wherever such a token is sent, the other tokens' results do not change by a bit."""
+    sh = SMALL.replace(T=21, F_shared=64)
+    inputs = make(sh, mixed)
+    layer = moe.DeviceLayer(inputs)
+    layer.quantize()
+    good = layer.decode(mx=mixed).clone()
+    layer.x[13] = bad
+    got = layer.decode(mx=mixed)
+    others = torch.arange(sh.T, device="cuda") != 13
+    assert torch.equal(got[others], good[others])
+    assert not torch.isfinite(got[13]).all()
+    idx = routing(layer)[0]
+    assert ((idx >= 0) & (idx < sh.E)).all()
+
+
 @pytest.mark.parametrize("mixed", [False, True])
 def test_weight_offsets_past_32_bits(mixed):
     """160 experts of 2048 x 7168: the last ones' weights lie past 2^31 values and, in bf16, past 2^32; a router bias
