@@ -12,7 +12,7 @@
 //   gate     one wave per token (gate_device.hpp); the workgroup that ends last makes the plan:
 //            the experts that have rows, in blocks of 16 of them, and their slots.  Per expert there is the
 //            64-bit mask of its tokens, so a slot's rank is a popcount and the order does not depend on
-//            the order of the writes
+//            the order of the writes.  (With up to four tokens there is no such launch: up does this for itself)
 //   up       a workgroup owns a block of rows of one expert and 16, 32 or 64 features (gate and up rows); its
 //            waves take 16 features each, or parts of K of the same ones
 //   down     the same on the other weights; float32 rows for each slot
@@ -27,8 +27,8 @@
 // Measured: 4 tokens on 8 experts of 4096 x 14336 in 4 bits, top-2, of which 5 to 7 are chosen: 101 - 119 us a call,
 // some 5 TB/s of weights; 64 tokens on 48 of 384 experts of 7168 x 2048 in 4 bits, top-8, and a shared expert: 210 us,
 // 4.1 TB/s (up 104 - 111 us, down 77 - 82, gate 13, logits 9.5, combine 4.5); one token, 128 experts of 2048 x 768 in
-// bf16, top-8: 37 us, of which the weights' stream is 16 at the rate of a copy and the five launches that wait for each other the
-// rest (up 15, down 7, gate 5, logits and combine 4 each).
+// bf16, top-8: 33 us, of which the weights' stream is 16 at the rate of a copy and the four launches that wait for each
+// other the rest.
 #include <algorithm>
 #include <cmath>
 
@@ -406,18 +406,69 @@ __device__ __forceinline__ void product(const Product& p, int split, int room, c
 }
 constexpr int kRedBytes = kWaves * 2 * 64 * 16;        // the parts' sums at most
 
+// A few tokens' gates and plan inside the up-projection: every workgroup chooses for itself, which takes less than a
+// launch.  All write the same choices; the one that is asked to leaves the plan for the launches behind it.
+constexpr int kOwnTokens = kWaves, kOwnSlots = 32;     // a wave per token, a lane per slot
+// entry a of the plan, its slots into s_slot; false: there is none.  s_key: kOwnTokens * 64 * PL floats.
+template <int PL>
+__device__ __forceinline__ bool own_entry(const DecodeProblem& p, int a, bool leave, float* s_key, int* s_slot, DecodePlan::Entry& own) {
+  __shared__ float s_gscore[kOwnTokens][64];
+  __shared__ int s_idx[kOwnSlots];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = p.T * p.top_k;
+  if (wave < p.T) {
+    const int e = gate_token<PL>(p.gate, wave, s_key + wave * 64 * PL, s_gscore[wave]);
+    if (lane < p.top_k) s_idx[wave * p.top_k + lane] = e;
+  }
+  __syncthreads();
+  // lane = slot; entries in the order of their first slots
+  const int cap = p.expert_capacity > 0 ? p.expert_capacity : kOwnTokens;
+  int e = lane < n ? s_idx[lane] - p.e_begin : -1;
+  if (e >= p.E_local) e = -1;
+  int rank = 0, all = 0, head = lane;
+  for (int j = n - 1; j >= 0; --j) {
+    const bool same = e >= 0 && __builtin_amdgcn_readlane(e, j) == e;
+    all += same;
+    rank += same && j < lane;
+    head = same ? j : head;
+  }
+  const uint64_t heads = __ballot(e >= 0 && head == lane), kept = __ballot(e >= 0 && rank < cap);
+  const int at = __popcll(heads & ((1ull << head) - 1)), count = min(all, cap);
+  if (leave && wave == 0) {
+    if (e >= 0 && head == lane) p.plan->entry[at] = DecodePlan::Entry{e, at * p.T, count, lane};
+    if (e >= 0 && rank < cap) p.plan->slot[at * p.T + rank] = lane;
+    if (__popcll(heads) + lane < decode_entries(p.T, p.top_k, p.E_local)) p.plan->entry[__popcll(heads) + lane].count = 0;
+    if (lane < p.T) p.plan->kept[lane] = (uint32_t)(kept >> (lane * p.top_k)) & ((1u << p.top_k) - 1);
+  }
+  const uint64_t mine = __ballot(e >= 0 && head == lane && at == a);
+  if (!mine) return false;                             // the whole workgroup
+  const int l = __builtin_ctzll(mine);
+  own.expert = __builtin_amdgcn_readlane(e, l);
+  own.count = __builtin_amdgcn_readlane(count, l);
+  own.first = l;
+  if (wave == 0 && e == own.expert && rank < cap) s_slot[rank] = lane;
+  __syncthreads();                                     // (the caller's LDS is free again, too)
+  return true;
+}
+
 // The shared expert's workgroups come first (16 tokens and some features each), then those of the plan's entries.
-template <bool MX, bool WHOLE>
+// PL > 0: the plan is own_entry's.
+template <bool MX, bool WHOLE, int PL>
 __global__ __launch_bounds__(64 * kWaves, MX ? 4 : 3) void k_decode_up(DecodeProblem p, Geometry g) {
   extern __shared__ __align__(16) char lds[];
+  __shared__ int s_slot[kOwnTokens];
   const int b = (int)blockIdx.x - g.shared, first = blockIdx.x / g.shared_tiles * 16;
   Product o{p.ws13, p.ws13_scales, p.x, 0, p.F_shared, p.d, p.F_shared,
             (int)(blockIdx.x % g.shared_tiles) * features_of(g.shared_split), min(16, p.T - first), nullptr, first, 1};
   bf16_t* act = p.act_shared;
   int split = g.shared_split;
   if (b >= 0) {
-    const DecodePlan::Entry e = p.plan->entry[b / g.tiles];
-    if (e.count == 0) return;
+    DecodePlan::Entry e;
+    if constexpr (PL > 0) {
+      if (!own_entry<PL>(p, b / g.tiles, b == 0, reinterpret_cast<float*>(lds), s_slot, e)) return;
+    } else {
+      e = p.plan->entry[b / g.tiles];
+      if (e.count == 0) return;
+    }
     split = g.split;
     o.w = p.w13;
     o.scales = p.w13_scales;
@@ -425,7 +476,7 @@ __global__ __launch_bounds__(64 * kWaves, MX ? 4 : 3) void k_decode_up(DecodePro
     o.row0 = (int64_t)e.expert * 2 * p.F;
     o.f0 = b % g.tiles * features_of(split);
     o.m = e.count;
-    o.slots = p.plan->slot + e.begin;
+    o.slots = PL > 0 ? s_slot : p.plan->slot + e.begin;
     o.first = e.first;
     o.per_token = p.top_k;
     act = p.act;
@@ -531,12 +582,35 @@ hipError_t launch_product(Kernel kernel, OccCache& cache, const DecodeProblem& p
   return hipGetLastError();
 }
 
-template <bool MX, bool WHOLE>
-hipError_t launch_up(const DecodeProblem& p, hipStream_t stream) {
+template <int PL>
+hipError_t launch_decode_gate(const DecodeProblem& p, hipStream_t stream) {
+  hipLaunchKernelGGL(k_decode_gate<PL>, dim3((p.T + 3) / 4), dim3(256), 0, stream, p);
+  return hipGetLastError();
+}
+
+template <bool MX, bool WHOLE, int PL>
+hipError_t launch_up(const DecodeProblem& p, const Geometry& g, size_t lds, hipStream_t stream) {
   static OccCache cache;
+  return launch_product(k_decode_up<MX, WHOLE, PL>, cache, p, g, lds, stream);
+}
+// the gate and the up-projection
+template <bool MX, bool WHOLE>
+hipError_t launch_gate_and_up(const DecodeProblem& p, hipStream_t stream) {
   size_t lds;
   const Geometry g = geometry(p, p.F, p.d, p.F_shared, p.d, 2, MX, lds);
-  return launch_product(k_decode_up<MX, WHOLE>, cache, p, g, lds, stream);
+  const int64_t blocks = (int64_t)decode_entries(p.T, p.top_k, p.E_local) * g.tiles;
+  // The gates in every workgroup, where there is a wave per token and a lane per slot, and all workgroups are on the chip
+  // at once and start with them: one token through 128 experts of 2048 x 768 in bf16 32.8 us a call against 36.0, through
+  // 48 of 7168 x 2048 in 4 bits with a shared expert 50.8 against 56.5; four tokens the same either way.
+  if (p.T <= kOwnTokens && p.T * p.top_k <= kOwnSlots && p.E <= 512 && blocks <= 4 * cu_count()) {
+    static_assert(kRedBytes >= kOwnTokens * 64 * 8 * 4, "keys of 512 experts in a launch's LDS");
+    return p.E <= 64 ? launch_up<MX, WHOLE, 1>(p, g, lds, stream) : p.E <= 128 ? launch_up<MX, WHOLE, 2>(p, g, lds, stream)
+           : p.E <= 256 ? launch_up<MX, WHOLE, 4>(p, g, lds, stream) : launch_up<MX, WHOLE, 8>(p, g, lds, stream);
+  }
+  const hipError_t e = p.E <= 64 ? launch_decode_gate<1>(p, stream) : p.E <= 128 ? launch_decode_gate<2>(p, stream)
+                       : p.E <= 256 ? launch_decode_gate<4>(p, stream) : p.E <= 512 ? launch_decode_gate<8>(p, stream)
+                                                                                    : launch_decode_gate<16>(p, stream);
+  return e != hipSuccess ? e : launch_up<MX, WHOLE, 0>(p, g, lds, stream);
 }
 template <bool MX, bool WHOLE>
 hipError_t launch_down(const DecodeProblem& p, hipStream_t stream) {
@@ -546,12 +620,6 @@ hipError_t launch_down(const DecodeProblem& p, hipStream_t stream) {
   return launch_product(k_decode_down<MX, WHOLE>, cache, p, g, lds, stream);
 }
 
-template <int PL>
-hipError_t launch_decode_gate(const DecodeProblem& p, hipStream_t stream) {
-  hipLaunchKernelGGL(k_decode_gate<PL>, dim3((p.T + 3) / 4), dim3(256), 0, stream, p);
-  return hipGetLastError();
-}
-
 template <bool MX>
 hipError_t launch_as(const DecodeProblem& p, hipStream_t stream) {
   const int splits = decode_logits_splits(p.E, p.d);
@@ -559,12 +627,8 @@ hipError_t launch_as(const DecodeProblem& p, hipStream_t stream) {
   hipLaunchKernelGGL(k_decode_logits, dim3((p.E + 15) / 16, (p.T + 15) / 16, splits), dim3(256), 0, stream, p, chunk);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  e = p.E <= 64 ? launch_decode_gate<1>(p, stream) : p.E <= 128 ? launch_decode_gate<2>(p, stream)
-      : p.E <= 256 ? launch_decode_gate<4>(p, stream) : p.E <= 512 ? launch_decode_gate<8>(p, stream)
-                                                                   : launch_decode_gate<16>(p, stream);
-  if (e != hipSuccess) return e;
   constexpr int UK = Unit<MX>::K;
-  e = p.d % UK == 0 ? launch_up<MX, true>(p, stream) : launch_up<MX, false>(p, stream);
+  e = p.d % UK == 0 ? launch_gate_and_up<MX, true>(p, stream) : launch_gate_and_up<MX, false>(p, stream);
   if (e != hipSuccess) return e;
   e = p.F % UK == 0 && p.F_shared % UK == 0 ? launch_down<MX, true>(p, stream) : launch_down<MX, false>(p, stream);
   if (e != hipSuccess) return e;

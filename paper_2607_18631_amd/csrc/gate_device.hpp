@@ -90,9 +90,10 @@ __device__ __forceinline__ float wave_max_fixed(float v) {
   return fmaxf(fmaxf(r0, r1), fmaxf(r2, r3));
 }
 
-// Token t of the problem, on the calling wave; s_key (64 * PL floats) and s_gscore (64) are the wave's own.
+// Token t of the problem, on the calling wave; s_key (64 * PL floats) and s_gscore (64) are the wave's own.  Lane r <
+// top_k gets slot r's expert.
 template <int PL>
-__device__ __forceinline__ void gate_token(const GateProblem& p, int64_t t, float* s_key, float* s_gscore) {
+__device__ __forceinline__ int gate_token(const GateProblem& p, int64_t t, float* s_key, float* s_gscore) {
   const int lane = threadIdx.x & 63;
 
   const int E = p.E;
@@ -279,6 +280,7 @@ __device__ __forceinline__ void gate_token(const GateProblem& p, int64_t t, floa
     p.topk_idx[t * p.top_k + lane] = oi;
     p.topk_w[t * p.top_k + lane] = ow;
   }
+  return oi;
 }
 
 }  // namespace moe

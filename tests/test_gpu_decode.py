@@ -159,6 +159,30 @@ def test_matches_the_layer():
     assert pu.rel_fro(b, a) <= 2 * pu.REL_TOL
 
 
+@pytest.mark.parametrize("mixed", [False, True])
+@pytest.mark.parametrize("T,kw", [
+    (1, dict(E=1, E_local=1, top_k=1)),
+    (4, dict(E=2, E_local=2, top_k=1)),                               # tokens that share experts
+    (4, dict(E=4, E_local=4, top_k=4, F_shared=96)),                  # every token chooses every expert
+    (4, dict(E=8, E_local=8, top_k=8)),                               # 32 slots
+    (3, dict(E=16, E_local=16, top_k=11)),                            # 33
+    (4, dict(E=16, E_local=16, top_k=16)),                            # 64
+    (3, dict(E=65, E_local=30, e_begin=20, top_k=5)),
+    (2, dict(E=130, E_local=130, top_k=6, gate=GATE_SIGMOID, routed_scale=2.5)),
+    (4, dict(E=256, E_local=256, top_k=8, gate=GATE_SIGMOID, n_group=8, topk_group=3)),
+    (4, dict(E=255, E_local=255, top_k=4, n_group=5, topk_group=2)),  # groups that are no runs of lanes
+    (1, dict(E=512, E_local=512, top_k=16)),
+    (2, dict(E=513, E_local=513, top_k=4)),
+    (2, dict(E=300, E_local=3, e_begin=297, top_k=2)),                # most likely nobody's expert
+    (4, dict(E=3, E_local=3, top_k=2, expert_capacity=1)),            # dropped slots
+    (4, dict(E=4, E_local=2, e_begin=1, top_k=3, expert_capacity=2, F_shared=32)),
+    (2, dict(E=16, E_local=16, top_k=4, d=512, F=4096)),              # more workgroups than are on the chip at once
+])
+def test_few_tokens_routing(T, kw, mixed):
+    """Up to a token per wave and a slot per lane the gates are made where they are used; and just past that."""
+    check(SMALL.replace(T=T, **kw), mixed)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), 3.0e38])
 @pytest.mark.parametrize("mixed", [False, True])
 def test_a_token_of_no_finite_values_stays_alone(bad, mixed):
