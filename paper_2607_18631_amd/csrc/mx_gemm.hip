@@ -12,14 +12,13 @@
 // stands before its last part.  There the whole slice is in registers, so its stage is free and takes the
 // copies of the slice STAGES further on; STAGES - 1 slices are on their way or landed.
 //
-// What bounds it: with many rows the matrix cores' power.  Bare loops of the instruction on random
-// operands run at 3.4 - 4.0 PFLOP/s (e4m3 rows) and 6.2 - 6.6 (e2m1), a fifth to a third below those on
-// zeros, and the clock in these kernels is 1.9 GHz; the rest is the share of LDS and L2 in that power and
-// the 5 us in which a tile begins and ends.  8192 rows on 8 experts of 4096 x 14336 in e2m1: 0.95 ms a
-// call, 3.1 PFLOP/s (0.83 ms with loads that are whole tiles; its products alone 0.44); 8192 on 32 of
-// 7168 x 2048 in e4m3: 0.45 ms (0.39; 0.21).  Of even loads of the latter, 416 us then: without the
-// products 344, without the copies 330, without LDS reads and copies 292.  With few rows it is the
-// weights' stream: 512 rows on the 32 experts 0.18 ms, 4.1 TB/s; 501 rows on 8 of 2048 x 1408 24 us.
+// What bounds it: with many rows the matrix cores, at the clock that their power leaves, and what shares it with them.
+// Bare loops of the instruction on random operands run at 3.4 - 4.0 PFLOP/s (e4m3 rows) and 6.2 - 6.6 (e2m1), a fifth to a
+// third below those on zeros.  Here they are busy for 63% and 48% of the cycles, at 1.9 GHz.  8192 rows on 8 experts of
+// 4096 x 14336 in e2m1: 0.95 ms a call, 3.1 PFLOP/s; with loads that are whole tiles 0.82, of which 0.18 go if nothing is
+// copied, 0.09 more if nothing is read from LDS, and 0.44 are the products of a bare loop; the rest are the 5 us in which a
+// tile begins and ends.  8192 rows on 32 of 7168 x 2048 in e4m3: 0.45 ms (0.39, 0.06, 0.04, 0.21).  With few rows it is the
+// weights' stream: 512 rows on the 32 experts 0.18 ms, 4.1 TB/s; 501 rows on 8 of 2048 x 1408 24 us, a chain of latencies.
 //
 // SwiGLU: two weight tiles of a wave are the gate and the up rows of the same 32 features, so the
 // activation and the maximum of its block are formed in registers, and the block leaves as elements and
@@ -213,19 +212,46 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
       h.x[m] = narrow(ld16(X + m * 32 * T::XROW));
     }
   };
-  auto read_scales = [&](int i, int j, Scales& s) {              // of slice i, parts j and j + 1
-    const char* S = s_scales + i / T::GROUP % 2 * (T::SROWS * 16) + (T::SLICE / 32 * i - group_start(i)) + 2 * j;
+  // The scales come to the registers 16 bytes of a row at a time, a group of slices: a word of each row, 16 bytes apart,
+  // takes LDS as long as all 16 (803 us a call against 813, of 1024 rows on each of 8 experts of 4096 x 14336 in e2m1; the
+  // same in e4m3).  Where a slice may end inside a row there are no registers left for that: word by word.
+  constexpr int HELD = WHOLE ? 4 : 1;
+  uint32_t held_w[NT][HELD], held_x[MT][HELD];
+  auto word_of = [&](int i, int j) { return (T::SLICE / 32 * i - group_start(i)) / 4 + j / 2; };   // parts j, j + 1 of slice i
+  auto read_scales = [&](int i, int j) {
+    const char* S = s_scales + i / T::GROUP % 2 * (T::SROWS * 16);
+    auto one = [&](int row, uint32_t (&v)[HELD]) {
+      if constexpr (WHOLE) {
+        const u32x4 r = ld16(S + row * 16);
 #pragma unroll
-    for (int n = 0; n < NT; ++n) s.w[n] = *reinterpret_cast<const int*>(S + (T::BM + wrow + n * 32) * 16);
+        for (int k = 0; k < 4; ++k) v[k] = r[k];
+      } else {
+        v[0] = *reinterpret_cast<const uint32_t*>(S + row * 16 + 4 * word_of(i, j));
+      }
+    };
 #pragma unroll
-    for (int m = 0; m < MT; ++m) s.x[m] = *reinterpret_cast<const int*>(S + (xrow + m * 32) * 16);
+    for (int n = 0; n < NT; ++n) one(T::BM + wrow + n * 32, held_w[n]);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) one(xrow + m * 32, held_x[m]);
   };
   // (apart from the read: a shift beside it would wait for it, and for the operands read before it)
-  auto own_scales = [&](const Scales& all, Scales& s) {
+  auto own_scales = [&](int i, int j, Scales& s) {
+    auto take = [&](auto kc) {
+      constexpr int k = decltype(kc)::value;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) s.w[n] = (uint32_t)all.w[n] >> (8 * q);
+      for (int n = 0; n < NT; ++n) s.w[n] = held_w[n][k] >> (8 * q);
 #pragma unroll
-    for (int m = 0; m < MT; ++m) s.x[m] = (uint32_t)all.x[m] >> (8 * q);
+      for (int m = 0; m < MT; ++m) s.x[m] = held_x[m][k] >> (8 * q);
+    };
+    if constexpr (WHOLE) {
+      const int k = word_of(i, j);
+      if (k == 0) take(std::integral_constant<int, 0>{});
+      else if (k == 1) take(std::integral_constant<int, 1>{});
+      else if (k == 2) take(std::integral_constant<int, 2>{});
+      else take(std::integral_constant<int, 3>{});
+    } else {
+      take(std::integral_constant<int, 0>{});
+    }
   };
   // One part's products, with the wave's other work between them: an instruction waits for those before it, so reads or
   // copies in one piece would leave the matrix core idle until the last of all eight waves' had been issued (930 us a
@@ -281,11 +307,11 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   else wait_vmcnt<0>();
   lds_barrier();
   Part part[2];
-  Scales s0, s1;
+  Scales s0;
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) read_step(ring[0], 0, i, part[0]);
-  read_scales(0, 0, s1);
-  own_scales(s1, s0);
+  read_scales(0, 0);
+  own_scales(0, 0, s0);
   // ring[0] holds slice s, ring[1] the next, ...
   int s = 0;
   // all parts of a slice but the last; `copy`: with the second half of the copies of the slice STAGES - 1 further on
@@ -294,10 +320,10 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
       constexpr int j = decltype(jc)::value;
       multiply(jc, part[j % 2], s0, [&](int i) {
         read_step(ring[0], j + 1, i, part[(j + 1) % 2]);
-        if (j % 2 && i == 0) read_scales(s, j + 1, s1);
+        if (!WHOLE && j % 2 && i == 0) read_scales(s, j + 1);
         if (PIECES > STEPS && j == 0 && copy) stage_piece(s + T::STAGES - 1, ring[T::STAGES - 1], STEPS + i);
       });
-      if (j % 2) own_scales(s1, s0);
+      if (j % 2) own_scales(s, j + 1, s0);
     };
     one(std::integral_constant<int, 0>{});
     if constexpr (T::PARTS > 2) {
@@ -312,10 +338,10 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     lds_barrier();                     // every wave's, and its reads of slice s
     multiply(last, part[1], s0, [&](int i) {
       read_step(ring[1], 0, i, part[0]);
-      if (i == 0) read_scales(s + 1, 0, s1);
+      if (i == 0 && (!WHOLE || (s + 1) % T::GROUP == 0)) read_scales(s + 1, 0);
       stage_piece(s + T::STAGES, ring[0], i);
     });
-    own_scales(s1, s0);
+    own_scales(s + 1, 0, s0);
     rotate();
   }
   for (; s < nk; ++s) {                // the last slices: nothing more to copy
@@ -324,9 +350,9 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     lds_barrier();
     multiply(last, part[1], s0, [&](int i) {
       read_step(ring[1], 0, i, part[0]);   // (behind the last slice: what lies there, not used)
-      if (i == 0) read_scales(min(s + 1, nk - 1), 0, s1);
+      if (i == 0 && (!WHOLE || (s + 1) % T::GROUP == 0)) read_scales(min(s + 1, nk - 1), 0);
     });
-    own_scales(s1, s0);
+    own_scales(min(s + 1, nk - 1), 0, s0);
     rotate();
   }
 
