@@ -3,7 +3,7 @@
 // Conversion.  A thread owns 8 neighbouring values (one 16-byte vector of bf16), a quad of lanes one
 // block of 32: the block's largest magnitude is two DPP exchanges away.  One pass over the data.
 //
-// Norm.  h = bf16(x + r), rstd = 1 / sqrt(mean(h^2) + eps), y = bf16(h rstd gamma): a row stays in
+// Norm.  h = bf16(x + r), rstd = 1 / sqrt(mean(h^2) + eps), y = bf16(h rstd gamma) rounded once: a row stays in
 // registers between its sum of squares and its scaling, so x and r are read once and h, y and the
 // 8-bit form of y are written once.  Rows of up to 2048 values belong to one wave (no barrier), longer
 // ones to a workgroup of 256 (one barrier); a row past 16384 values is read again from h.
@@ -14,7 +14,7 @@
 //
 // All of them are bound by memory.  Measured (bytes read and written over the time; a large copy runs at 4.8 TB/s):
 // conversion of 131072 x 7168 to e2m1 and back 839 us, 5.1 TB/s; norm of 8192 x 7168 with both results 97 us, 5.5 TB/s;
-// norm and backward of 16384 x 2048 104 us, 4.5 TB/s, of 3001 x 2040 28 us (three launches), 3.0 TB/s; one row 4.2 us,
+// norm and backward of 16384 x 2048 104 us, 4.5 TB/s, of 3001 x 2040 28 us (three launches), 3.0 TB/s; one row 4.5 us,
 // a launch.
 #include "common.hpp"
 #include "kernels.hpp"
@@ -106,30 +106,68 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantize(MxConvertProblem p) 
 }
 
 // ---------------- norm ----------------
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
 // Sum over the threads of a row: a wave (TPR = 64), or the workgroup through LDS (one slot per wave,
 // two sets used in turn so that consecutive calls need one barrier each).
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float* s_part, int set) {
+template <int TPR, class F>
+__device__ __forceinline__ F row_sum(F v, F* s_part, int set) {
   v = wave_sum(v);
   if constexpr (TPR > 64) {
     constexpr int NW = TPR / 64;
-    float* q = s_part + set * NW;
+    F* q = s_part + set * NW;
     if ((threadIdx.x & 63) == 0) q[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = 0.f;
+    v = 0;
 #pragma unroll
     for (int w = 0; w < NW; ++w) v += q[w];
   }
   return v;
 }
 
+// Forward statistics: the sum of squares and rstd in float64, so that y can be right to the last bit.  Float32 products
+// decide its bf16, but for those within their error of a border between two (one in 4096), which float64 decides.  A
+// block's 8-bit form turns on that bit: its scale doubles where its largest value rounds up to a power of two, and all 32
+// elements change with it.  (Hidden behind the memory: 8192 rows of 7168 98 us, in float32 alone 97; one wave a row is 1 us
+// longer, 10.8 against 9.6 with 3001 rows of 2040.)
+__device__ __forceinline__ double row_rstd(double sum, const AddNormProblem& p) {
+  return 1.0 / sqrt(sum / p.d + (double)p.eps);
+}
+// within 8 units of float32's last place of the middle between two bf16 values (three roundings of half a unit, and rstd's)
+__device__ __forceinline__ bool near_border(float y) { return (__float_as_uint(y) & 0xffffu) - 0x7ff8u <= 16u; }
+// y moved to the side of that middle on which exact lies
+__device__ __forceinline__ float settle(float y, double exact) {
+  const uint32_t middle = (__float_as_uint(y) & 0xffff0000u) | 0x8000u;
+  const double m = fabs((double)__uint_as_float(middle)), e = fabs(exact);
+  return __uint_as_float(e > m ? middle + 1 : e < m ? middle - 1 : middle);
+}
+
 // scaled values of one vector: y and its 8-bit form
-__device__ __forceinline__ void norm_store(const AddNormProblem& p, int64_t at, const float (&f)[8], float rstd,
+__device__ __forceinline__ void norm_store(const AddNormProblem& p, int64_t at, const float (&f)[8], double rstd,
                                            u32x4 gamma, bool live) {
   float g[8], y[8];
   unpack8(gamma, g);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) y[j] = f[j] * rstd * g[j];
+  for (int j = 0; j < 8; ++j) y[j] = f[j] * (float)rstd * g[j];
+  uint32_t near = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) near |= near_border(y[j]) ? 1u << j : 0u;
+  while (near) {                                              // one at a time: little code, and hardly ever two
+    const int k = __builtin_ctz(near);
+    float yk = y[0], fg = f[0] * g[0];                        // (16 significant bits: exact)
+#pragma unroll
+    for (int j = 1; j < 8; ++j) {
+      yk = j == k ? y[j] : yk;
+      fg = j == k ? f[j] * g[j] : fg;
+    }
+    yk = settle(yk, fg * rstd);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = j == k ? yk : y[j];
+    near &= near - 1;
+  }
   const u32x4 yb = pack8(y);
   if (live && p.y) st16(p.y + at, yb);
   if (p.y_q) {
@@ -147,7 +185,7 @@ __device__ __forceinline__ void norm_store(const AddNormProblem& p, int64_t at, 
 template <int TPR, int VPT>
 __global__ __launch_bounds__(kThreads) void k_add_norm(AddNormProblem p) {
   constexpr int RPB = kThreads / TPR;
-  __shared__ float s_part[2 * (kThreads / 64)];
+  __shared__ double s_part[2 * (kThreads / 64)];
   const int t = threadIdx.x % TPR;
   const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
   if (row >= p.rows) return;                                  // whole waves (TPR = 64), or the whole workgroup
@@ -161,7 +199,7 @@ __global__ __launch_bounds__(kThreads) void k_add_norm(AddNormProblem p) {
     if (p.residual) b[i] = ld16(p.residual + at + v * 8);
     gm[i] = ld16(p.gamma + v * 8);
   }
-  float sq = 0.f;
+  double sq = 0;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int v = t + i * TPR;
@@ -178,11 +216,11 @@ __global__ __launch_bounds__(kThreads) void k_add_norm(AddNormProblem p) {
       float f[8];
       unpack8(a[i], f);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sq = fmaf(f[j], f[j], sq);
+      for (int j = 0; j < 8; ++j) sq = fma((double)f[j], (double)f[j], sq);
     }
   }
-  const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, s_part, 0) / (float)p.d + p.eps);
-  if (p.rstd && t == 0) p.rstd[row] = rstd;
+  const double rstd = row_rstd(row_sum<TPR>(sq, s_part, 0), p);
+  if (p.rstd && t == 0) p.rstd[row] = (float)rstd;
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int v = t + i * TPR;
@@ -195,11 +233,11 @@ __global__ __launch_bounds__(kThreads) void k_add_norm(AddNormProblem p) {
 // rows too long for the registers of a workgroup: h (or x) is read a second time, each vector by the
 // thread that wrote it
 __global__ __launch_bounds__(kThreads) void k_add_norm_long(AddNormProblem p) {
-  __shared__ float s_part[2 * (kThreads / 64)];
+  __shared__ double s_part[2 * (kThreads / 64)];
   const int64_t row = blockIdx.x;
   const int nv = p.d / 8;
   const int64_t at = row * p.d;
-  float sq = 0.f;
+  double sq = 0;
   for (int v = threadIdx.x; v < nv; v += kThreads) {
     float f[8];
     u32x4 a = ld16(p.x + at + (int64_t)v * 8);
@@ -214,10 +252,10 @@ __global__ __launch_bounds__(kThreads) void k_add_norm_long(AddNormProblem p) {
       unpack8(a, f);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sq = fmaf(f[j], f[j], sq);
+    for (int j = 0; j < 8; ++j) sq = fma((double)f[j], (double)f[j], sq);
   }
-  const float rstd = 1.0f / sqrtf(row_sum<kThreads>(sq, s_part, 0) / (float)p.d + p.eps);
-  if (p.rstd && threadIdx.x == 0) p.rstd[row] = rstd;
+  const double rstd = row_rstd(row_sum<kThreads>(sq, s_part, 0), p);
+  if (p.rstd && threadIdx.x == 0) p.rstd[row] = (float)rstd;
   const bf16_t* src = p.residual ? p.h : p.x;
   // whole quads per round: the lanes past the row take part in the block maxima
   for (int v0 = 0; v0 < nv; v0 += kThreads) {
