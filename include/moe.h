@@ -388,8 +388,8 @@ int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, co
 /* Residual addition and RMS norm in front of a layer, row by row:
  *     h = bf16(x + residual),  rstd = 1 / sqrt(mean(h^2) + eps),  y = bf16(h * rstd * gamma),
  *     (y_q, y_scales) = moe_mx_quantize(y) in E4M3,
- * statistics in float64, y rounded once.  x, residual, h, y [rows, d] bf16; gamma [d] bf16; rstd [rows] f32;
- * y_q, y_scales [rows, d] in E4M3.
+ * statistics in float64; y is the bf16 of the float32 nearest to the float64 product.  x, residual,
+ * h, y [rows, d] bf16; gamma [d] bf16; rstd [rows] f32; y_q, y_scales [rows, d] in E4M3.
  *   residual NULL: h is x itself, nothing is added and h must be NULL.  Otherwise h is required; it
  *                  may be x's or residual's own buffer.
  *   y, or y_q and y_scales together, may be NULL (not wanted), not all three; rstd may be NULL.

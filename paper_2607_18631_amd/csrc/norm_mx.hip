@@ -3,7 +3,7 @@
 // Conversion.  A thread owns 8 neighbouring values (one 16-byte vector of bf16), a quad of lanes one
 // block of 32: the block's largest magnitude is two DPP exchanges away.  One pass over the data.
 //
-// Norm.  h = bf16(x + r), rstd = 1 / sqrt(mean(h^2) + eps), y = bf16(h rstd gamma) rounded once: a row stays in
+// Norm.  h = bf16(x + r), rstd = 1 / sqrt(mean(h^2) + eps), y = bf16(h rstd gamma): a row stays in
 // registers between its sum of squares and its scaling, so x and r are read once and h, y and the
 // 8-bit form of y are written once.  Rows of up to 2048 values belong to one wave (no barrier), longer
 // ones to a workgroup of 256 (one barrier); a row past 16384 values is read again from h.
@@ -13,7 +13,7 @@
 // each workgroup leaves one row of partial sums, which a second kernel adds in a fixed order.
 //
 // All of them are bound by memory.  Measured (bytes read and written over the time; a large copy runs at 4.8 TB/s):
-// conversion of 131072 x 7168 to e2m1 and back 839 us, 5.1 TB/s; norm of 8192 x 7168 with both results 97 us, 5.5 TB/s;
+// conversion of 131072 x 7168 to e2m1 and back 839 us, 5.1 TB/s; norm of 8192 x 7168 with both results 98 us, 5.4 TB/s;
 // norm and backward of 16384 x 2048 104 us, 4.5 TB/s, of 3001 x 2040 28 us (three launches), 3.0 TB/s; one row 4.5 us,
 // a launch.
 #include "common.hpp"
@@ -128,23 +128,16 @@ __device__ __forceinline__ F row_sum(F v, F* s_part, int set) {
   return v;
 }
 
-// Forward statistics: the sum of squares and rstd in float64, so that y can be right to the last bit.  Float32 products
-// decide its bf16, but for those within their error of a border between two (one in 4096), which float64 decides.  A
-// block's 8-bit form turns on that bit: its scale doubles where its largest value rounds up to a power of two, and all 32
-// elements change with it.  (Hidden behind the memory: 8192 rows of 7168 98 us, in float32 alone 97; one wave a row is 1 us
-// longer, 10.8 against 9.6 with 3001 rows of 2040.)
+// Forward statistics: the sum of squares and rstd in float64, so that y is the bf16 of the float64 result's float32.
+// Float32 products decide it, but for those within their error of a border between two bf16 values (one in 4096), which
+// are taken again in float64.  A block's 8-bit form turns on that bit: its scale doubles where its largest value rounds up
+// to a power of two, and all 32 elements change with it.  (Hidden behind the memory: 8192 rows of 7168 98 us, in float32
+// alone 97; one wave a row is 1 us longer, 10.8 against 9.6 with 3001 rows of 2040.)
 __device__ __forceinline__ double row_rstd(double sum, const AddNormProblem& p) {
   return 1.0 / sqrt(sum / p.d + (double)p.eps);
 }
 // within 8 units of float32's last place of the middle between two bf16 values (three roundings of half a unit, and rstd's)
 __device__ __forceinline__ bool near_border(float y) { return (__float_as_uint(y) & 0xffffu) - 0x7ff8u <= 16u; }
-// y moved to the side of that middle on which exact lies
-__device__ __forceinline__ float settle(float y, double exact) {
-  const uint32_t middle = (__float_as_uint(y) & 0xffff0000u) | 0x8000u;
-  const double m = fabs((double)__uint_as_float(middle)), e = fabs(exact);
-  return __uint_as_float(e > m ? middle + 1 : e < m ? middle - 1 : middle);
-}
-
 // scaled values of one vector: y and its 8-bit form
 __device__ __forceinline__ void norm_store(const AddNormProblem& p, int64_t at, const float (&f)[8], double rstd,
                                            u32x4 gamma, bool live) {
@@ -157,13 +150,10 @@ __device__ __forceinline__ void norm_store(const AddNormProblem& p, int64_t at, 
   for (int j = 0; j < 8; ++j) near |= near_border(y[j]) ? 1u << j : 0u;
   while (near) {                                              // one at a time: little code, and hardly ever two
     const int k = __builtin_ctz(near);
-    float yk = y[0], fg = f[0] * g[0];                        // (16 significant bits: exact)
+    float fg = f[0] * g[0];                                   // (16 significant bits: exact)
 #pragma unroll
-    for (int j = 1; j < 8; ++j) {
-      yk = j == k ? y[j] : yk;
-      fg = j == k ? f[j] * g[j] : fg;
-    }
-    yk = settle(yk, fg * rstd);
+    for (int j = 1; j < 8; ++j) fg = j == k ? f[j] * g[j] : fg;
+    const float yk = (float)(fg * rstd);
 #pragma unroll
     for (int j = 0; j < 8; ++j) y[j] = j == k ? yk : y[j];
     near &= near - 1;

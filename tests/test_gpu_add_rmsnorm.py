@@ -102,19 +102,15 @@ def test_forward_options(d):
 
 
 @pytest.mark.parametrize("rows,d", [(40000, 64), (3000, 2048), (2000, 7168), (200, 16416)])
-def test_every_value_is_the_nearest(rows, d):
-    """No neighbour of a result in bf16 is nearer to the float64 value: the 8-bit form's scale turns on that."""
+def test_every_value_is_the_float64_one(rows, d):
+    """The float64 result to float32 to bf16, in every bit: the 8-bit form's scale turns on the last."""
     g = torch.Generator(device="cuda").manual_seed(rows)
     x, r = (torch.empty((rows, d), device="cuda").normal_(generator=g).to(BF16) for _ in range(2))
     gamma = (torch.empty(d, device="cuda").normal_(generator=g) * 0.3 + 1).to(BF16)
     h, y = torch.empty_like(x), torch.empty_like(x)
     moe.moe_add_rmsnorm(x, r, gamma, 1e-5, h, y)
     want = h.double() / (h.double().pow(2).mean(1, keepdim=True) + float(np.float32(1e-5))).sqrt() * gamma.double()
-    off = (y.double() - want).abs()
-    for side in (float("inf"), -float("inf")):
-        neighbour = torch.nextafter(y, torch.full_like(y, side)).double()
-        # (float64's own error at a tie: none is so near by chance)
-        assert ((neighbour - want).abs() >= off * (1 - 2.0 ** -40)).all()
+    assert torch.equal(y, want.float().to(BF16))
 
 
 @pytest.mark.parametrize("d", [64, 2048, 7168, 16416])
