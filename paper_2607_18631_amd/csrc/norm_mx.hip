@@ -10,7 +10,8 @@
 //
 // Norm backward.  With u = h rstd, g = dy gamma: dx = rstd (g - u mean(g u)) + dh, and dgamma = sum over
 // rows of dy u.  A wave or workgroup walks rows and keeps the dgamma sums of its columns in registers;
-// each workgroup leaves one row of partial sums, which a second kernel adds in a fixed order.
+// each workgroup leaves one row of partial sums, which a second kernel adds in a fixed order (a single workgroup writes
+// dgamma itself).
 //
 // All of them are bound by memory.  Measured (bytes read and written over the time; a large copy runs at 4.8 TB/s):
 // conversion of 131072 x 7168 to e2m1 and back 839 us, 5.1 TB/s; norm of 8192 x 7168 with both results 98 us, 5.4 TB/s;
@@ -320,7 +321,8 @@ __global__ __launch_bounds__(kThreads) void k_add_norm_bwd(AddNormBwdProblem p) 
       }
     }
   }
-  // the workgroup's partial sums
+  // the workgroup's partial sums; of the only workgroup, the result
+  const bool only = gridDim.x == 1;
   float* part = p.parts + (int64_t)blockIdx.x * p.d;
   if constexpr (RPB > 1) {
     // the waves' sums of the same columns, added in wave order
@@ -336,14 +338,19 @@ __global__ __launch_bounds__(kThreads) void k_add_norm_bwd(AddNormBwdProblem p) 
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < RPB; ++w) s += s_dg[w][(c % 8) * TPR + c / 8];
-        if (col < p.d) part[col] = s;
+        if (col < p.d) {
+          if (only) p.dgamma[col] = (bf16_t)f32_to_bf16(s);
+          else part[col] = s;
+        }
       }
     }
   } else {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
       const int v = t + i * TPR;
-      if (v < nv) {
+      if (v < nv && only) {
+        st16(p.dgamma + v * 8, pack8(dg[i]));
+      } else if (v < nv) {
         *reinterpret_cast<f32x4*>(part + v * 8) = f32x4{dg[i][0], dg[i][1], dg[i][2], dg[i][3]};
         *reinterpret_cast<f32x4*>(part + v * 8 + 4) = f32x4{dg[i][4], dg[i][5], dg[i][6], dg[i][7]};
       }
@@ -522,7 +529,8 @@ hipError_t launch_add_norm_bwd(const AddNormBwdProblem& p, hipStream_t stream) {
     else hipLaunchKernelGGL(k_add_norm_bwd_long<false>, dim3(parts), dim3(kThreads), 0, stream, p);
     e = hipGetLastError();
   }
-  if (e != hipSuccess) return e;
+  // (one workgroup's sums are the result: a launch less for up to 16 rows)
+  if (e != hipSuccess || (parts == 1 && p.d <= kBlockRow)) return e;
   hipLaunchKernelGGL(k_dgamma, dim3((p.d + 31) / 32), dim3(kThreads), 0, stream, p.parts, parts, p.d, p.dgamma);
   return hipGetLastError();
 }
