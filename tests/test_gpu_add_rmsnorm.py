@@ -209,6 +209,12 @@ def test_backward_rows(rows):
     run_backward(rows, 264)
 
 
+@pytest.mark.parametrize("rows,d", [(1, 2056), (2, 2056), (3, 2056), (255, 2056), (257, 4104), (4100, 2056), (3, 16416), (300, 16416)])
+def test_backward_long_rows(rows, d):
+    """One workgroup, a workgroup per row, and several rows each."""
+    run_backward(rows, d)
+
+
 def test_backward_in_place_and_repeatable():
     for d in (512, 7168):
         a = run_backward(300, d)
