@@ -98,7 +98,6 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   constexpr int MINE = (T::NX + T::NW + T::WAVES - 1) / T::WAVES, LEAST = (T::NX + T::NW) / T::WAVES;
   constexpr int SMINE = (T::NS + T::WAVES - 1) / T::WAVES;
   uint32_t from[MINE];
-  int kofs[MINE];                                              // first K value of a copy
   const char* sfrom[SMINE];
   const int64_t wrow0 = (int64_t)g * (SWIGLU ? 2 * (int64_t)N : N);
   // weight row (from the group's first) of the stage's row i: plain, or per wave 32 gate and 32 up rows
@@ -120,12 +119,10 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     if (id < T::NX) {
       const int byte = id * 1024 + lane * 16, r = byte / T::XROW, ch = mx_chunk<T::XROW>(r, (byte % T::XROW) / 16);
       from[c] = (uint32_t)(min(r, rows - 1) * xbytes) + ch * 16;
-      kofs[c] = ch * (FMT == MX_E4M3 ? 16 : 32);
     } else {
       const int byte = (min(id, T::NX + T::NW - 1) - T::NX) * 1024 + lane * 16, r = byte / T::WROW;
       const int ch = mx_chunk<T::WROW>(r, (byte % T::WROW) / 16);
       from[c] = (uint32_t)(weight_row(r) * wbytes) + ch * 16;
-      kofs[c] = ch * 32;
     }
   }
 #pragma unroll
@@ -133,11 +130,26 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     const int r = (wave + c * T::WAVES) * 64 + lane;
     sfrom[c] = r < T::BM ? xs + (int64_t)min(r, rows - 1) * KB : ws + (int64_t)weight_row(min(r - T::BM, T::BN - 1)) * KB;
   }
+  const char* x_end = (const char*)p.X_scales + p.max_rows * KB;
+  const char* w_end = (const char*)p.W_scales + (int64_t)p.groups * (SWIGLU ? 2 * (int64_t)N : N) * KB;
+  // the slice's value with which this lane's chunks begin, for all its copies: their chunks repeat every 16 rows
+  static_assert(WHOLE || (T::WAVES * 1024 / T::XROW % 16 == 0 && 1024 / T::WROW % 16 == 0), "whole periods between copies");
+  auto first_value = [&](bool x) {
+    int l = lane;
+    asm volatile("" : "+v"(l));                                // found again where it is used: in no register of the loop
+    return x ? mx_chunk<T::XROW>((wave * 1024 + l * 16) / T::XROW, l * 16 % T::XROW / 16) * (FMT == MX_E4M3 ? 16 : 32)
+             : mx_chunk<T::WROW>(l * 16 / T::WROW, l * 16 % T::WROW / 16) * 32;
+  };
   // Scales: a row's 4 bytes of one slice are as many cache accesses and requests as its 64 or 128 bytes of values, so
-  // they come for 512 values at a time: 16 bytes per row.  Where rows end inside the last group's 16 bytes, it starts
-  // that much earlier.  (WHOLE rows have 16 scales at least.)
+  // they come for a group of slices at a time: 16 bytes per row.  Where rows end inside the last group's 16 bytes, it
+  // starts that much earlier.  (WHOLE rows have 16 scales at least.)  Rows that start at any byte are copied from the
+  // word that holds their group's first: 16 bytes then hold 3 slices' 12 wherever those start in them.  (Loaded byte by
+  // byte they kept every copy behind them waiting: 8192 rows on 32 experts of 4128 x 2080 in e4m3 370 us a call against 518;
+  // of 4096 x 2048 273.)
+  constexpr int GROUP = WHOLE ? T::GROUP : 3;
+  static_assert(WHOLE || (T::SLICE == 128 && T::STAGES <= GROUP + 1), "words of 4 blocks, and two sets");
   char* s_scales = smem + T::STAGES * T::STAGE;
-  auto group_start = [&](int s) { return WHOLE ? min(s / T::GROUP * 16, KB - 16) : s / T::GROUP * 16; };   // block
+  auto group_start = [&](int s) { return WHOLE ? min(s / GROUP * 16, KB - 16) : s / GROUP * 12; };   // block
   // A stage's copies in pieces, each issued behind two tiles' products: STEPS of them in a slice's last part, and where
   // there are many, as many more in the next slice's first (256 rows in e4m3 397 us a call against 420, of 8192 rows
   // on 32 experts of 7168 x 2048; smaller tiles lose a little, 178 against 175 with 512 rows).
@@ -151,27 +163,37 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
       const bool x = id < T::NX;
       const char* b = x ? xb + s * T::XROW : wb + s * T::WROW;
       bf16_t* dst = (bf16_t*)(base + id * 1024);
-      if constexpr (WHOLE) {
+      if (WHOLE || (s + 1) * T::SLICE <= K) {                  // (uniform)
         dma16_sv(b, from[c], dst);
       } else {
-        dma16_v(s * T::SLICE + kofs[c] < K ? b + from[c] : (const char*)g_zero_chunk, dst);
+        dma16_v(s * T::SLICE + first_value(x) < K ? b + from[c] : (const char*)g_zero_chunk, dst);
       }
     }
-    if (piece == STEPS - 1 && s % T::GROUP == 0) {
-      char* set = s_scales + s / T::GROUP % 2 * (T::SROWS * 16);
+    if (piece == STEPS - 1 && s % GROUP == 0) {
+      char* set = s_scales + s / GROUP % 2 * (T::SROWS * 16);
+      const int at = group_start(s);
 #pragma unroll
       for (int c = 0; c < SMINE; ++c) {
         const int id = wave + c * T::WAVES;
-        if (id < T::NS) {
-          if constexpr (WHOLE) {
-            dma16_v(sfrom[c] + group_start(s), (bf16_t*)(set + id * 1024));
-          } else {
-            // scales past the row's end are zeros, never the next row's bytes (255 would make NaN of zeros)
-            u32x4 v = {0, 0, 0, 0};
+        if (id >= T::NS) continue;
+        if constexpr (WHOLE) {
+          dma16_v(sfrom[c] + at, (bf16_t*)(set + id * 1024));
+        } else {
+          const int first = (int)((uintptr_t)sfrom[c] & 3);
+          const char* word = sfrom[c] - first + at;
+          const bool past = word + 16 > (id * 64 + lane < T::BM ? x_end : w_end);
+          dma16_v(past ? (const char*)g_zero_chunk : word, (bf16_t*)(set + id * 1024));
+          if (__ballot(past)) {                                // the tensor's last rows: byte by byte
+            wait_vmcnt<0>();
+            if (past) {
+              u32x4 v = {0, 0, 0, 0};
+              for (int j = 0; j < 12 && at + j < KB; ++j) {
+                const uint32_t s = (uint32_t)(uint8_t)sfrom[c][at + j] << (8 * ((first + j) % 4));
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-              if (group_start(s) + j < KB) v[j / 4] |= (uint32_t)(uint8_t)sfrom[c][group_start(s) + j] << (8 * (j % 4));
-            *reinterpret_cast<u32x4*>(set + id * 1024 + lane * 16) = v;
+                for (int k = 0; k < 4; ++k) v[k] |= (first + j) / 4 == k ? s : 0u;
+              }
+              *reinterpret_cast<u32x4*>(set + id * 1024 + lane * 16) = v;
+            }
           }
         }
       }
@@ -214,19 +236,24 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   };
   // The scales come to the registers 16 bytes of a row at a time, a group of slices: a word of each row, 16 bytes apart,
   // takes LDS as long as all 16 (803 us a call against 813, of 1024 rows on each of 8 experts of 4096 x 14336 in e2m1; the
-  // same in e4m3).  Where a slice may end inside a row there are no registers left for that: word by word.
-  constexpr int HELD = WHOLE ? 4 : 1;
+  // same in e4m3).  For rows that start at any byte it is the two words that hold a slice's four.
+  constexpr int HELD = WHOLE ? 4 : 2;
   uint32_t held_w[NT][HELD], held_x[MT][HELD];
+  // where in its word a row's group starts (the same for rows 32 apart)
+  const int first_w = WHOLE ? 0 : (int)((uintptr_t)(ws + (int64_t)weight_row(wrow) * KB) & 3);
+  const int first_x = WHOLE ? 0 : (int)((uintptr_t)(xs + (int64_t)xrow * KB) & 3);
   auto word_of = [&](int i, int j) { return (T::SLICE / 32 * i - group_start(i)) / 4 + j / 2; };   // parts j, j + 1 of slice i
   auto read_scales = [&](int i, int j) {
-    const char* S = s_scales + i / T::GROUP % 2 * (T::SROWS * 16);
+    const char* S = s_scales + i / GROUP % 2 * (T::SROWS * 16);
     auto one = [&](int row, uint32_t (&v)[HELD]) {
       if constexpr (WHOLE) {
         const u32x4 r = ld16(S + row * 16);
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = r[k];
       } else {
-        v[0] = *reinterpret_cast<const uint32_t*>(S + row * 16 + 4 * word_of(i, j));
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(S + row * 16) + word_of(i, j);
+        v[0] = w[0];
+        v[1] = w[1];
       }
     };
 #pragma unroll
@@ -236,21 +263,27 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
   };
   // (apart from the read: a shift beside it would wait for it, and for the operands read before it)
   auto own_scales = [&](int i, int j, Scales& s) {
-    auto take = [&](auto kc) {
-      constexpr int k = decltype(kc)::value;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) s.w[n] = held_w[n][k] >> (8 * q);
-#pragma unroll
-      for (int m = 0; m < MT; ++m) s.x[m] = held_x[m][k] >> (8 * q);
-    };
     if constexpr (WHOLE) {
+      auto take = [&](auto kc) {
+        constexpr int k = decltype(kc)::value;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) s.w[n] = held_w[n][k] >> (8 * q);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) s.x[m] = held_x[m][k] >> (8 * q);
+      };
       const int k = word_of(i, j);
       if (k == 0) take(std::integral_constant<int, 0>{});
       else if (k == 1) take(std::integral_constant<int, 1>{});
       else if (k == 2) take(std::integral_constant<int, 2>{});
       else take(std::integral_constant<int, 3>{});
     } else {
-      take(std::integral_constant<int, 0>{});
+      // blocks past the row's end are zeros, never the next row's (255 would make NaN of zeros)
+      const int left = KB - 4 * i;
+      const uint32_t exist = left >= 4 ? ~0u : (1u << (8 * left)) - 1;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s.w[n] = (__builtin_amdgcn_alignbyte(held_w[n][1], held_w[n][0], first_w) & exist) >> (8 * q);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) s.x[m] = (__builtin_amdgcn_alignbyte(held_x[m][1], held_x[m][0], first_x) & exist) >> (8 * q);
     }
   };
   // One part's products, with the wave's other work between them: an instruction waits for those before it, so reads or
@@ -338,7 +371,7 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     lds_barrier();                     // every wave's, and its reads of slice s
     multiply(last, part[1], s0, [&](int i) {
       read_step(ring[1], 0, i, part[0]);
-      if (i == 0 && (!WHOLE || (s + 1) % T::GROUP == 0)) read_scales(s + 1, 0);
+      if (i == 0 && (!WHOLE || (s + 1) % GROUP == 0)) read_scales(s + 1, 0);
       stage_piece(s + T::STAGES, ring[0], i);
     });
     own_scales(s + 1, 0, s0);
@@ -350,7 +383,7 @@ __device__ __forceinline__ void mx_tile(const MxGemmProblem& p, char* smem, int 
     lds_barrier();
     multiply(last, part[1], s0, [&](int i) {
       read_step(ring[1], 0, i, part[0]);   // (behind the last slice: what lies there, not used)
-      if (i == 0 && (!WHOLE || (s + 1) % T::GROUP == 0)) read_scales(min(s + 1, nk - 1), 0);
+      if (i == 0 && (!WHOLE || (s + 1) % GROUP == 0)) read_scales(min(s + 1, nk - 1), 0);
     });
     own_scales(min(s + 1, nk - 1), 0, s0);
     rotate();

@@ -184,6 +184,16 @@ def test_mlp_widths(fmt, d, F):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d,F", [(32, 64), (416, 224), (608, 736), (640, 1056), (1312, 544)])
+def test_mlp_rows_whose_scales_start_at_any_byte(fmt, d, F):
+    """Rows of 1 to 41 scales, so that they start at every byte of a word and end past every one; the rows around an
+    expert's, in the equal-stride layout, have NaN scales, and so has every weight row of an expert without rows."""
+    run_mlp(fmt, d, F, [3, 0, 70, 1, 17, 129])
+    run_mlp(fmt, d, F, [2, 5, 0, 7], capacity=7, seed=1)
+    run_mlp(fmt, d, F, [1])                                            # the tensors end with the row
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("counts", [[1], [0, 1, 0], [31, 32, 33], [64, 65, 127, 2], [130, 0, 128, 129, 1],
                                     [255, 256, 257], [600, 3, 0, 511]])
 def test_mlp_rows(fmt, counts):
