@@ -14,7 +14,7 @@
 //
 // What bounds it: with many rows the matrix cores, at the clock that their power leaves, and what shares it with them.
 // Bare loops of the instruction on random operands run at 3.4 - 4.0 PFLOP/s (e4m3 rows) and 6.2 - 6.6 (e2m1), a fifth to a
-// third below those on zeros.  Here they are busy for 63% and 48% of the cycles, at 1.9 GHz.  8192 rows on 8 experts of
+// third below those on zeros.  Here they are busy for 62% and 48% of the cycles, at 1.9 GHz, LDS for 19% and 22%.  8192 rows on 8 experts of
 // 4096 x 14336 in e2m1: 0.95 ms a call, 3.1 PFLOP/s; with loads that are whole tiles 0.82, of which 0.18 go if nothing is
 // copied, 0.09 more if nothing is read from LDS, and 0.44 are the products of a bare loop; the rest are the 5 us in which a
 // tile begins and ends.  8192 rows on 32 of 7168 x 2048 in e4m3: 0.45 ms (0.39, 0.06, 0.04, 0.21).  With few rows it is the
