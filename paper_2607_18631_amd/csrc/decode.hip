@@ -421,7 +421,8 @@ __device__ __forceinline__ bool own_entry(const DecodeProblem& p, int a, bool le
   }
   __syncthreads();
   // lane = slot; entries in the order of their first slots
-  const int cap = p.expert_capacity > 0 ? p.expert_capacity : kOwnTokens;
+  // (a token chooses an expert once, so an expert has a row per token at most: s_slot holds them)
+  const int cap = p.expert_capacity > 0 ? min(p.expert_capacity, kOwnTokens) : kOwnTokens;
   int e = lane < n ? s_idx[lane] - p.e_begin : -1;
   if (e >= p.E_local) e = -1;
   int rank = 0, all = 0, head = lane;

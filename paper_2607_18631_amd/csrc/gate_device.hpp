@@ -7,7 +7,7 @@
 // lower expert index, so the result does not depend on lane scheduling.
 //
 // Top-k, one expert per round: every key is mapped to a 32-bit unsigned integer with the same
-// order (chosen and ineligible experts map to 0, below every key), the wave maximum of the lanes'
+// order (order_key.hpp; chosen and ineligible experts map to 0, below every key), the wave maximum of the lanes'
 // largest values is taken with DPP moves (no LDS traffic), and of the lanes holding it the lowest
 // lane wins (a ballot), inside it the lowest expert: equal keys go to the lower expert index.
 //
@@ -22,19 +22,9 @@
 
 #include "common.hpp"
 #include "kernels.hpp"
+#include "order_key.hpp"
 
 namespace moe {
-
-// float -> uint32 with the same order (finite values and infinities; -0 counts as +0)
-__device__ __forceinline__ uint32_t ordered(float f) {
-  const uint32_t u = __float_as_uint(f + 0.0f);
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-
-// the float key back from its ordered image (inverse of ordered)
-__device__ __forceinline__ float unordered(uint32_t o) {
-  return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
-}
 
 // lanes of the rows in ROWS take src from the DPP pattern CTRL, the others 0 (the identity of an
 // unsigned maximum, so each step below is one v_max_u32 with a DPP operand)
@@ -249,7 +239,7 @@ __device__ __forceinline__ int gate_token(const GateProblem& p, int64_t t, float
 #pragma unroll
     for (int j = PL - 2; j >= 0; --j) jf = (uk[j] == m) ? j : jf;
     const int jw = __builtin_amdgcn_readlane(jf, wl);
-    // (the host guarantees at least top_k eligible experts, so m names one)
+    // (the host guarantees at least top_k eligible experts and no key maps to 0, so m names one not chosen yet)
     oi = lane == r ? min(wl * PL + jw, E - 1) : oi;
     okey = lane == r ? unordered(m) : okey;
     first = r == 0 ? unordered(m) : first;
