@@ -129,36 +129,21 @@ __device__ __forceinline__ F row_sum(F v, F* s_part, int set) {
   return v;
 }
 
-// Forward statistics: the sum of squares and rstd in float64, so that y is the bf16 of the float64 result's float32.
-// Float32 products decide it, but for those within their error of a border between two bf16 values (one in 4096), which
-// are taken again in float64.  A block's 8-bit form turns on that bit: its scale doubles where its largest value rounds up
-// to a power of two, and all 32 elements change with it.  (Hidden behind the memory: 8192 rows of 7168 98 us, in float32
-// alone 97; one wave a row is 1 us longer, 10.8 against 9.6 with 3001 rows of 2040.)
+// Forward: the sum of squares, rstd and the product in float64, so that y is the bf16 of the float64 result's float32 for
+// rows of any finite size (float32 has no room for h * gamma of large rows, or for rstd of subnormal ones).  A block's 8-bit
+// form turns on y's last bit: its scale doubles where its largest value rounds up to a power of two, and all 32 elements
+// change with it.  (Hidden behind the memory, and as fast as float32 products with a second, float64 look at those next to a
+// border between two bf16 values: 8192 rows of 7168 99 us either way, one row 4.2 against 4.4, 3001 of 2040 10.6 against 10.7.)
 __device__ __forceinline__ double row_rstd(double sum, const AddNormProblem& p) {
   return 1.0 / sqrt(sum / p.d + (double)p.eps);
 }
-// within 8 units of float32's last place of the middle between two bf16 values (three roundings of half a unit, and rstd's)
-__device__ __forceinline__ bool near_border(float y) { return (__float_as_uint(y) & 0xffffu) - 0x7ff8u <= 16u; }
 // scaled values of one vector: y and its 8-bit form
 __device__ __forceinline__ void norm_store(const AddNormProblem& p, int64_t at, const float (&f)[8], double rstd,
                                            u32x4 gamma, bool live) {
   float g[8], y[8];
   unpack8(gamma, g);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) y[j] = f[j] * (float)rstd * g[j];
-  uint32_t near = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) near |= near_border(y[j]) ? 1u << j : 0u;
-  while (near) {                                              // one at a time: little code, and hardly ever two
-    const int k = __builtin_ctz(near);
-    float fg = f[0] * g[0];                                   // (16 significant bits: exact)
-#pragma unroll
-    for (int j = 1; j < 8; ++j) fg = j == k ? f[j] * g[j] : fg;
-    const float yk = (float)(fg * rstd);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = j == k ? yk : y[j];
-    near &= near - 1;
-  }
+  for (int j = 0; j < 8; ++j) y[j] = (float)((double)f[j] * (double)g[j] * rstd);   // (f g is exact)
   const u32x4 yb = pack8(y);
   if (live && p.y) st16(p.y + at, yb);
   if (p.y_q) {
