@@ -75,12 +75,12 @@ template <bool MX, bool WHOLE>
 struct WeightUnit {
   u32x4 v[MX ? 2 : 4];
 
-  // this lane's part of the unit at k0 of 16 rows of K values; not `on`: nothing is read
-  __device__ __forceinline__ void load(Buffer w, int r, int q, int k0, int K, bool on = true) {
+  // this lane's part of the unit at k0 of 16 rows of K values: zeros from `end` on; not `on`: nothing is read
+  __device__ __forceinline__ void load(Buffer w, int r, int q, int k0, int K, int end, bool on = true) {
 #pragma unroll
     for (int i = 0; i < (MX ? 2 : 4); ++i) {
       const int k = frag_k<MX>(MX ? 4 * i : i, q);
-      v[i] = load16(w, on && (WHOLE || k0 + k < K) ? (MX ? (r * K + k) / 2 : 2 * (r * K + k)) : kPast,
+      v[i] = load16(w, on && (WHOLE || k0 + k < end) ? (MX ? (r * K + k) / 2 : 2 * (r * K + k)) : kPast,
                                   MX ? k0 / 2 : 2 * k0);
     }
   }
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256) void k_decode_logits(DecodeProblem p, int chun
     for (int i = 0; i < IN_FLIGHT; ++i) {
       const int k = min(k0 + i * UK, p.d - 1) / 8 * 8;             // inside the row, past `end` or not
       const int stop = k0 + i * UK < end ? end : 0;
-      u[i].load(w, r, q, k, p.d);                             // (weights past `end` meet zeros)
+      u[i].load(w, r, q, k, p.d, stop);                       // (neither side past `end`: an infinity times 0 is NaN)
       b[i].load(x, row, q, k, stop);
     }
 #pragma unroll
@@ -303,7 +303,7 @@ __device__ __forceinline__ void multiply(const Product& p, int slot, int f0w, in
   auto load = [&](Stage& st, int i) {
     const int u = min(part + split * i, units - 1);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) st.w[s].load(w[s], r, q, u * UK, K, i < count);
+    for (int s = 0; s < NS; ++s) st.w[s].load(w[s], r, q, u * UK, K, K, i < count);
   };
 
   // ---- LDS: the scales of all the workgroup's weight rows, then its token rows, as many rounds of K at a time as
