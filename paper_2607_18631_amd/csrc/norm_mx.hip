@@ -107,6 +107,7 @@ __global__ __launch_bounds__(kThreads) void k_mx_dequantize(MxConvertProblem p) 
 }
 
 // ---------------- norm ----------------
+using moe::wave_sum;                                          // (float32: a sum of another type would hide it)
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
