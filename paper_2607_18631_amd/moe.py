@@ -240,6 +240,14 @@ def _bytes(device, name, t, n):
     return t.data_ptr()
 
 
+def _rows_of(device, name, t, rows, n):
+    """Pointer of a contiguous uint8 tensor of exactly ``rows`` rows of n values: flat, or with rows as its last dimension."""
+    if t is None or t.dtype is not _u8 or t.numel() != rows * n or t.device != device or not t.is_contiguous() or (
+            t.dim() > 1 and t.shape[-1] != n):
+        _mismatch(device, name, t, _u8, f"of {rows} rows of {n} values")
+    return t.data_ptr()
+
+
 def _ws(device, ws):
     """(pointer, bytes) of a workspace."""
     return (None, 0) if ws is None else (_bytes(device, "ws", ws, 0), ws.numel())
@@ -294,15 +302,15 @@ def moe_mx_dequantize(format, elements, scales, x, stream=None):
 
 
 def moe_mx_grouped_ffn(sh, format, x_q, x_scales, offsets, w13_q, w13_scales, w2_q, w2_scales, y_perm, ws, stream=None):
-    """The expert MLP on block-scaled rows in expert order (``format``) and e2m1 weights.  ``x_q`` / ``x_scales`` and
-    ``y_perm`` have ``sh.capacity`` rows; ``offsets`` is ``moe_permute``'s, or with an expert capacity its counts."""
+    """The expert MLP on block-scaled rows in expert order (``format``) and e2m1 weights (flat, or rows as their last
+    dimension).  ``y_perm`` has ``sh.capacity`` rows, ``x_q`` and ``x_scales`` at least as many; ``offsets`` is ``moe_permute``'s, or with an expert capacity its counts."""
     d, F, El, cap = sh.d, sh.F, sh.E_local, sh.capacity
     dev = _matrix("y_perm", y_perm)[2]
     _on(dev, stream, _lib.moe_mx_grouped_ffn, ctypes.byref(shape_c(sh)), format,
         _bytes(dev, "x_q", x_q, cap * mx_elements_per_row(format, d)), _bytes(dev, "x_scales", x_scales, cap * (d // 32)),
         _take(dev, "offsets", offsets, _i32, El if sh.expert_capacity > 0 else El + 1),
-        _bytes(dev, "w13_q", w13_q, El * F * d), _bytes(dev, "w13_scales", w13_scales, El * 2 * F * (d // 32)),
-        _bytes(dev, "w2_q", w2_q, El * d * F // 2), _bytes(dev, "w2_scales", w2_scales, El * d * (F // 32)),
+        _rows_of(dev, "w13_q", w13_q, El * 2 * F, d // 2), _rows_of(dev, "w13_scales", w13_scales, El * 2 * F, d // 32),
+        _rows_of(dev, "w2_q", w2_q, El * d, F // 2), _rows_of(dev, "w2_scales", w2_scales, El * d, F // 32),
         _take(dev, "y_perm", y_perm, _bf16, cap, d), *_ws(dev, ws))
 
 
@@ -349,7 +357,7 @@ def moe_layer_decode(sh, x, w_router, bias, w13, w2, ws13, ws2, out, ws, scales=
 
     def weights(name, t, s, rows, K):
         if scales is not None:
-            return _bytes(dev, name, t, rows * K // 2), _bytes(dev, name + "_scales", s, rows * (K // 32))
+            return _rows_of(dev, name, t, rows, K // 2), _rows_of(dev, name + "_scales", s, rows, K // 32)
         if t is None or t.dtype is not _bf16 or t.numel() != rows * K or t.device != dev or not t.is_contiguous():
             _mismatch(dev, name, t, _bf16, f"of {rows * K} values")
         return t.data_ptr(), None
