@@ -32,6 +32,7 @@
 #include "gemm_device.hpp"
 #include "kernels.hpp"
 #include "mx_device.hpp"
+#include "mx_tile_rule.hpp"
 
 namespace moe {
 namespace {
@@ -556,43 +557,28 @@ hipError_t launch_as(const MxGemmProblem& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Slices of 256 values where the token rows are e2m1 and every slice is whole: rows of 128 bytes are one cache line
-// each, rows of 64 cost as many accesses for half the bytes (2048 rows on 8 experts of 4096 x 14336: 395 us a call
-// against 444; 8192 rows: 841 against 874).  e4m3 rows have 128 bytes in slices of 128, and LDS has no room for two
-// such stages of 256 rows.
 template <int FMT, int WM, int WN, int MT, int NT>
 hipError_t launch_tile(const MxGemmProblem& p, hipStream_t stream) {
+  const MxSlices slices = mx_slices(FMT == MX_E2M1, WN * NT * 32, p.K);
   if constexpr (FMT == MX_E2M1 && WN * NT == 8) {
-    if (p.K % 256 == 0 && p.K >= 512) {
+    if (slices == MxSlices::kWhole256) {
       using T = MxTile<FMT, WM, WN, MT, NT, 3, 256>;
       return p.swiglu ? launch_as<T, true, true>(p, stream) : launch_as<T, false, true>(p, stream);
     }
   }
-  // whole: no slice has a row's end inside, and a row has the scales of a group
   using T = MxTile<FMT, WM, WN, MT, NT, 4, 128>;
-  const bool whole = p.K % 128 == 0 && p.K >= 512;
+  const bool whole = slices == MxSlices::kWhole128;
   if (p.swiglu) return whole ? launch_as<T, true, true>(p, stream) : launch_as<T, true, false>(p, stream);
   return whole ? launch_as<T, false, true>(p, stream) : launch_as<T, false, false>(p, stream);
 }
 
-// Rows x weight rows of a tile, by the rows that a group has in the mean (the loads themselves stay on the device):
-//   256 x 256  where groups have more than 64 rows and the tiles fill the chip.  The weights are read once for a group's
-//              130 rows: 8192 rows on 64 experts of 2048 x 1408 in e2m1 120 us a call against 149 with 128 rows.
-//   128 x 128  where such tiles fit on the chip at once: a tile waits for its slices' latency, so more compute units
-//              asking is more memory at work.  501 rows on 8 experts of 2048 x 1408 in e4m3 26 us against 32 with
-//              128 x 256; but 2048 rows on 4 of 2048 x 1024, which take a second round, 45 against 35.
-//   128 x 256  elsewhere: that case 35 us against 51 with 256 rows; 512 rows on 32 experts of 7168 x 2048 in e2m1 153
-//              against 168, as a low tile of 64 rows has more slices on their way.
-// (Slower everywhere: 32 and 64 rows with 4 waves, which have nobody on their SIMD to multiply while they read.)
 template <int FMT>
 hipError_t launch_format(const MxGemmProblem& p, hipStream_t stream) {
-  const int64_t per_group = p.max_rows / p.groups;
-  const int64_t weight_rows = (int64_t)p.N * (p.swiglu ? 2 : 1), chip = cu_count();
-  // (a group ends half a tile early in the mean)
-  const int64_t narrow = p.groups * ((per_group + 64 + 127) / 128) * ((weight_rows + 127) / 128);
-  const int64_t large = p.groups * ((per_group + 255) / 256) * ((weight_rows + 255) / 256);
-  if (narrow <= chip) return launch_tile<FMT, 4, 2, 1, 2>(p, stream);
-  return per_group > 64 && large >= chip ? launch_tile<FMT, 4, 2, 2, 4>(p, stream) : launch_tile<FMT, 2, 4, 2, 2>(p, stream);
+  switch (mx_tile_rule(cu_count(), p.max_rows, p.groups, p.N * (p.swiglu ? int64_t(2) : int64_t(1)))) {
+    case MxTileId::k128x128: return launch_tile<FMT, 4, 2, 1, 2>(p, stream);
+    case MxTileId::k256x256: return launch_tile<FMT, 4, 2, 2, 4>(p, stream);
+    default: return launch_tile<FMT, 2, 4, 2, 2>(p, stream);
+  }
 }
 
 }  // namespace
