@@ -378,8 +378,9 @@ int moe_mx_dequantize(int64_t rows, int32_t cols, int format, const void* elemen
  *    w13_q, w13_scales  [E_local * 2F, d]    E2M1, the rows as in w13
  *    w2_q, w2_scales    [E_local * d, F]     E2M1, the rows as in w2
  *    y_perm             [cap, d] bf16; rows outside every segment are not written
- * Limits beside moe_grouped_ffn's: d and F multiples of 32 below 2^20, d * F < 2^31.  Offsets, layouts
- * and clamping as there.
+ * Limits beside moe_grouped_ffn's: d and F multiples of 32 below 2^20, d * F < 2^31; a product of 2^23
+ * tiles (128 rows by 256 weight rows) or more is refused as a launch (MOE_ERR_HIP).  Offsets, layouts and
+ * clamping as there.
  * ws: MOE_WS_MX_FFN bytes. */
 int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, const void* x_scales,
                        const int32_t* offsets, const void* w13_q, const void* w13_scales, const void* w2_q,
@@ -394,7 +395,8 @@ int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, co
  *                  may be x's or residual's own buffer.
  *   y, or y_q and y_scales together, may be NULL (not wanted), not all three; rstd may be NULL.
  *   eps >= 0 and finite.  A row of zeros with eps = 0 gives NaN.
- * No output but h may overlap an input.  d a multiple of 8, of 32 where y_q is given; rows >= 0. */
+ * No output but h may overlap an input.  d a multiple of 8 up to 2^31 - 32, of 32 where y_q is given;
+ * 0 <= rows < 2^31. */
 int moe_add_rmsnorm(int64_t rows, int32_t d, float eps, const void* x, const void* residual, const void* gamma,
                     void* h, void* y, void* y_q, void* y_scales, float* rstd, void* stream);
 
@@ -418,7 +420,8 @@ size_t moe_add_rmsnorm_workspace_size(int64_t rows, int32_t d);
  * the elements, their values enter the products exactly, and x and the activation stay bf16.  Either
  * way the router and x are bf16.  Honours expert_capacity; ignores fusion.
  * d, F and F_shared are below 2^20; with E2M1 they are multiples of 32, d <= 16384 and F, F_shared <=
- * 32768.  The chosen experts and their gates are left at the start of the workspace, at the offsets
+ * 32768.  The experts' rows in blocks of 16, times max(d, F) / 64, are below 2^24 (1024 experts with rows
+ * and d, F < 2^19 always are).  The chosen experts and their gates are left at the start of the workspace, at the offsets
  * moe_workspace_offset gives for MOE_REGION_TOPK_IDX and MOE_REGION_TOPK_W.  Deterministic.  Calls that
  * may overlap need a workspace each.
  * ws: MOE_WS_DECODE bytes. */

@@ -38,6 +38,14 @@ inline int check_decode_shape(const moe_shape_t* s) {
   // 32-bit byte offsets into 16 weight rows and into the activations of every slot
   const int32_t widest = s->d > s->F ? (s->d > s->F_shared ? s->d : s->F_shared) : (s->F > s->F_shared ? s->F : s->F_shared);
   if (widest >= (1 << 20)) return fail(MOE_ERR_UNSUPPORTED, "d, F or F_shared (%d) >= 2^20", widest);
+  // a launch has less than 2^32 threads: 256 for 64 features of each entry of the plan where there are so many, and for 32
+  // of 16 tokens of the shared expert
+  const int64_t features = s->d > s->F ? s->d : s->F, shared = s->F_shared > s->d ? s->F_shared : s->d;
+  const int64_t blocks = decode_entries((int)s->T, s->top_k, s->E_local) * ((features + 63) / 64) +
+                         (s->F_shared > 0 ? (s->T + 15) / 16 * ((shared + 31) / 32) : 0);
+  if (blocks >= (int64_t(1) << 24))
+    return fail(MOE_ERR_UNSUPPORTED, "d or F (%lld) makes 2^24 workgroups or more (%lld) of %d experts' rows",
+                (long long)features, (long long)blocks, decode_entries((int)s->T, s->top_k, s->E_local));
   return MOE_OK;
 }
 

@@ -44,6 +44,8 @@ int check_norm_sizes(int64_t rows, int32_t d) {
   if (rows >= (int64_t(1) << 31)) return fail(MOE_ERR_UNSUPPORTED, "rows (%lld) >= 2^31", (long long)rows);
   if (d <= 0) return fail(MOE_ERR_INVALID_ARG, "d (%d) <= 0", d);
   if (d % 8) return fail(MOE_ERR_UNSUPPORTED, "d (%d) %% 8 != 0 (rows must be 16-byte bf16 vectors)", d);
+  // column numbers are 32 bits wide, a workgroup's 32 columns of dgamma from the last whole 32 on included
+  if (d > INT32_MAX - 31) return fail(MOE_ERR_UNSUPPORTED, "d (%d) > 2^31 - 32", d);
   return MOE_OK;
 }
 
