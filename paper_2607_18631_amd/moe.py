@@ -437,17 +437,19 @@ class DeviceLayer:
         return g
 
     def quantize(self):
-        """The expert weights in e2m1 for ``decode(mx=True)``: per tensor (elements, scales)."""
+        """The expert weights in e2m1 for ``decode(mx=True)``: per tensor (elements, scales).  Called again, after the
+        weights changed, it writes the same buffers, so a graph captured on them reads the new weights."""
         import torch
-        self.mx = {}
+        held, made = getattr(self, "mx", None) or {}, {}
         for name in ("w13", "w2", "ws13", "ws2"):
             w = getattr(self, name)
             if w is not None:
                 rows, cols = w.numel() // w.shape[-1], w.shape[-1]
-                q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=self.device)
-                s = torch.empty((rows, cols // 32), dtype=torch.uint8, device=self.device)
+                q, s = held[name] if name in held else (torch.empty((rows, n), dtype=torch.uint8, device=self.device)
+                                                        for n in (cols // 2, cols // 32))
                 moe_mx_quantize(MOE_MX_E2M1, w.view(rows, cols), q, s)
-                self.mx[name] = (q, s)
+                made[name] = (q, s)
+        self.mx = made
         return self.mx
 
     def decode(self, mx: bool = False, stream=None):
