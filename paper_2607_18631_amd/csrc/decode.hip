@@ -549,15 +549,27 @@ Geometry geometry(const DecodeProblem& p, int features, int K, int features_s, i
   Geometry g{};
   auto tiles = [](int features, int split) { return (features + features_of(split) - 1) / features_of(split); };
   // Waves on the same features: fewer where there are many workgroups (rows staged once serve more weights), more
-  // where there are few.  The shared expert's rows are all the tokens; its workgroups come first.
+  // where there are few.  `waves`: of 16 features each, one wave on them.  The up-projection's, which stream two rows of
+  // weights, are shared out longer than the down-projection's.  Measured in us a call, for 1 / 2 / 4 waves, weights from memory:
+  //   up    128 waves (1 token, 48 of 384 experts of 7168 x 2048 in 4 bits) 36.4 / 29.8 / 27.0; 384 (1 token, 128 of 2048 x 768)
+  //         bf16 36.7 / 29.9 / 32.3, 4 bits 24.2 / 22.9 / 23.4; 952 (8 tokens of the first) 66 / 60 / 63; 4900 (4 tokens, 8 of
+  //         4096 x 14336) 105 / 101 / 101, in bf16 415 / 385 / 364; 6045 (64 tokens of the second) in bf16 253 / 240 / 244;
+  //         7168 (64 tokens, 8 of 4096 x 14336) 250 / 278 / 338, in bf16 679 / 698 / 699
+  //   down  512 (1 token, 8 of 4096 x 14336) 54 / 46.5 / 45.5; 1024 23.3 / 23.3 / 24.2; 1400 105 / 101 / 101; 3333 58 / 62 / 71;
+  //         6607 49 / 52 / 60; 10541 128 / 132 / 153; 16121 102 / 119 / 153
+  // The shared expert's rows are all the tokens; its workgroups come first.  2 waves: 4 of 2048 x 2816 in 4 bits with 1
+  // token 25.0 / 22.6 / 22.6, 64 tokens 119 / 123 / 130; 7168 x 2048 with 8 tokens 74 / 62 / 63, 64 tokens 208 / 217 / 237.
   const double waves = expected_active(p) * ((features + 15) / 16);
-  g.split = waves >= 8192 ? 1 : waves >= 512 ? 2 : 4;
+  g.split = waves >= (ns == 2 ? 7000 : 3000) ? 1 : waves >= (ns == 2 ? 256 : 768) ? 2 : 4;
   g.shared_split = 2;
   g.tiles = tiles(features, g.split);
   g.shared_tiles = std::max(1, tiles(features_s, g.shared_split));
   g.shared = p.F_shared ? g.shared_tiles * ((p.T + 15) / 16) : 0;
   // LDS: scales, and rows: room for all of an expert's rows where that leaves four workgroups per compute unit, else
-  // as much as leaves two.  A round of the most rows has to fit.
+  // as much as leaves two.  A round of the most rows has to fit.  (38 KB / 76 KB where the mean is above 1.25 rows: long rows
+  // gain from 76, 16 of 14336 values each in the down-projection 307 / 278 us a call, 16 tokens through a shared expert of
+  // 7168 x 2048 and 32 of 256 experts 107 / 91; short ones lose, 4 rows of 2048 in the up-projection 91 / 102, 2 of 2048 in the
+  // down-projection 204 / 218.  At 1.0 to 1.1 rows they are the same but for rows of 7168, 62 / 60.)
   const int widest = std::max(K, p.F_shared ? K_s : 0), split = std::max(g.split, g.shared_split);
   const int64_t fixed = mx ? (int64_t)ns * std::max(features_of(g.split), features_of(g.shared_split)) * (widest / 32) : 0;
   const double rows = (double)p.T * p.top_k / p.E * p.E_local / expected_active(p);
