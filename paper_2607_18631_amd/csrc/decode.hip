@@ -29,10 +29,8 @@
 // 4.1 TB/s (up 104 - 111 us, down 77 - 82, gate 13, logits 9.5, combine 4.5); one token, 128 experts of 2048 x 768 in
 // bf16, top-8: 33 us, of which the weights' stream is 16 at the rate of a copy and the four launches that wait for each
 // other the rest.
-#include <algorithm>
-#include <cmath>
-
 #include "common.hpp"
+#include "decode_geometry.hpp"
 #include "gate_device.hpp"
 #include "gemm_device.hpp"
 #include "kernels.hpp"
@@ -41,14 +39,16 @@
 namespace moe {
 namespace {
 
+using Geometry = DecodeGeometry;
+
 // an offset past every buffer (they end below it)
 constexpr uint32_t kPast = 0x80000000u;
 
 // K values of a unit: the operand fragments of 32 values whose loads a wave issues together.
 template <bool MX>
 struct Unit {
-  static constexpr int FRAGS = MX ? 8 : 4;
-  static constexpr int K = 32 * FRAGS;
+  static constexpr int K = decode_unit(MX);
+  static constexpr int FRAGS = K / 32;
 };
 
 // Lane (r = l % 16, q = l / 16) holds 8 values of row r in fragment f of a unit; which 8 is free as long
@@ -239,22 +239,10 @@ __global__ __launch_bounds__(256) void k_decode_gate(DecodeProblem p) {
 }
 
 // ---------------- the experts' products ----------------
-constexpr int kWaves = 4;
+constexpr int kWaves = kDecodeWaves;
 // units of weights a wave has on their way
 template <bool MX>
 constexpr int kStages = MX ? 4 : 3;
-
-// One launch's geometry: `split` waves share the same 16 features (each takes every split-th unit of K), so a
-// workgroup owns 16 * kWaves / split features; `room` bytes of LDS hold rows.
-struct Geometry {
-  int32_t tiles, shared_tiles;     // workgroups per entry of the plan, per 16 tokens of the shared expert
-  int32_t shared;                  // workgroups of the shared expert
-  int32_t split, shared_split, room;
-};
-__host__ __device__ constexpr int features_of(int split) { return 16 * kWaves / split; }
-// bytes between rows of K values in LDS: 16 past the row, so that the four rows and four q's that a read touches at
-// once lie in different banks
-__host__ __device__ constexpr int row_bytes(int K) { return 2 * K + 16; }
 
 // What a workgroup multiplies: m rows of `rows` (row_at(i) bytes into it) by weight rows [row0, ..) of K values,
 // NS streams (gate and up) of them `stream` rows apart.
@@ -404,7 +392,6 @@ __device__ __forceinline__ void product(const Product& p, int split, int room, c
   }
   if (part == 0 && r < p.m && f0w + 4 * q < p.features) done(slot, f0w + 4 * q, acc);
 }
-constexpr int kRedBytes = kWaves * 2 * 64 * 16;        // the parts' sums at most
 
 // A few tokens' gates and plan inside the up-projection: every workgroup chooses for itself, which takes less than a
 // launch.  All write the same choices; the one that is asked to leaves the plan for the launches behind it.
@@ -538,60 +525,19 @@ __global__ __launch_bounds__(256) void k_decode_combine(DecodeProblem p) {
 }
 
 // ---------------- launches ----------------
-// experts that have rows when every token chooses at random (geometry only)
-double expected_active(const DecodeProblem& p) {
-  const double none = std::pow(1.0 - (double)p.top_k / p.E, p.T);
-  return std::max(1.0, p.E_local * (1.0 - none));
-}
-
 // `features` x K weights of each expert, ns streams of them (`features_s` x K_s of the shared expert)
-Geometry geometry(const DecodeProblem& p, int features, int K, int features_s, int K_s, int ns, bool mx, size_t& lds) {
-  Geometry g{};
-  auto tiles = [](int features, int split) { return (features + features_of(split) - 1) / features_of(split); };
-  // Waves on the same features: fewer where there are many workgroups (rows staged once serve more weights), more
-  // where there are few.  `waves`: of 16 features each, one wave on them.  The up-projection's, which stream two rows of
-  // weights, are shared out longer than the down-projection's.  Measured in us a call, for 1 / 2 / 4 waves, weights from memory:
-  //   up    128 waves (1 token, 48 of 384 experts of 7168 x 2048 in 4 bits) 36.4 / 29.8 / 27.0; 384 (1 token, 128 of 2048 x 768)
-  //         bf16 36.7 / 29.9 / 32.3, 4 bits 24.2 / 22.9 / 23.4; 952 (8 tokens of the first) 66 / 60 / 63; 4900 (4 tokens, 8 of
-  //         4096 x 14336) 105 / 101 / 101, in bf16 415 / 385 / 364; 6045 (64 tokens of the second) in bf16 253 / 240 / 244;
-  //         7168 (64 tokens, 8 of 4096 x 14336) 250 / 278 / 338, in bf16 679 / 698 / 699
-  //   down  512 (1 token, 8 of 4096 x 14336) 54 / 46.5 / 45.5; 1024 23.3 / 23.3 / 24.2; 1400 105 / 101 / 101; 3333 58 / 62 / 71;
-  //         6607 49 / 52 / 60; 10541 128 / 132 / 153; 16121 102 / 119 / 153
-  // The shared expert's rows are all the tokens; its workgroups come first.  2 waves: 4 of 2048 x 2816 in 4 bits with 1
-  // token 25.0 / 22.6 / 22.6, 64 tokens 119 / 123 / 130; 7168 x 2048 with 8 tokens 74 / 62 / 63, 64 tokens 208 / 217 / 237.
-  const double waves = expected_active(p) * ((features + 15) / 16);
-  g.split = waves >= (ns == 2 ? 7000 : 3000) ? 1 : waves >= (ns == 2 ? 256 : 768) ? 2 : 4;
-  g.shared_split = 2;
-  g.tiles = tiles(features, g.split);
-  g.shared_tiles = std::max(1, tiles(features_s, g.shared_split));
-  g.shared = p.F_shared ? g.shared_tiles * ((p.T + 15) / 16) : 0;
-  // LDS: scales, and rows: room for all of an expert's rows where that leaves four workgroups per compute unit, else
-  // as much as leaves two.  A round of the most rows has to fit.  (38 KB / 76 KB where the mean is above 1.25 rows: long rows
-  // gain from 76, 16 of 14336 values each in the down-projection 307 / 278 us a call, 16 tokens through a shared expert of
-  // 7168 x 2048 and 32 of 256 experts 107 / 91; short ones lose, 4 rows of 2048 in the up-projection 91 / 102, 2 of 2048 in the
-  // down-projection 204 / 218.  At 1.0 to 1.1 rows they are the same but for rows of 7168, 62 / 60.)
-  const int widest = std::max(K, p.F_shared ? K_s : 0), split = std::max(g.split, g.shared_split);
-  const int64_t fixed = mx ? (int64_t)ns * std::max(features_of(g.split), features_of(g.shared_split)) * (widest / 32) : 0;
-  const double rows = (double)p.T * p.top_k / p.E * p.E_local / expected_active(p);
-  const int most = std::min(p.T, 16);
-  const int64_t least = (int64_t)most * row_bytes(std::min(split * (mx ? Unit<true>::K : Unit<false>::K), widest));
-  const int64_t all = (int64_t)most * row_bytes((widest + split * 256 - 1) / (split * 256) * (split * 256));
-  const int64_t room = std::max(least, (rows > 1.25 ? 76 : 38) * 1024 - fixed);
-  g.room = (int)std::min(room, std::max(all, least));
-  lds = (size_t)std::max<int64_t>(kRedBytes, g.room + fixed);
-  return g;
+Geometry geometry(const DecodeProblem& p, int features, int K, int features_s, int K_s, int ns, bool mx) {
+  return decode_geometry({p.T, p.E, p.E_local, p.top_k, p.F_shared > 0}, features, K, features_s, K_s, ns, mx);
 }
 
-constexpr size_t kMostLds = 158 * 1024;
 template <class Kernel>
-hipError_t launch_product(Kernel kernel, OccCache& cache, const DecodeProblem& p, const Geometry& g, size_t lds,
-                          hipStream_t stream) {
-  if (lds > kMostLds) return hipErrorInvalidValue;
+hipError_t launch_product(Kernel kernel, OccCache& cache, const DecodeProblem& p, const Geometry& g, hipStream_t stream) {
+  if (g.lds > kDecodeMostLds) return hipErrorInvalidValue;
   // (the limit of 64 KiB of dynamic LDS is raised once per device and kernel)
   hipError_t err = hipSuccess;
-  if (kernel_occupancy(cache, reinterpret_cast<const void*>(kernel), 64 * kWaves, kMostLds, err) <= 0) return err;
+  if (kernel_occupancy(cache, reinterpret_cast<const void*>(kernel), 64 * kWaves, kDecodeMostLds, err) <= 0) return err;
   const int64_t blocks = g.shared + (int64_t)decode_entries(p.T, p.top_k, p.E_local) * g.tiles;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kWaves), lds, stream, p, g);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(64 * kWaves), g.lds, stream, p, g);
   return hipGetLastError();
 }
 
@@ -602,35 +548,33 @@ hipError_t launch_decode_gate(const DecodeProblem& p, hipStream_t stream) {
 }
 
 template <bool MX, bool WHOLE, int PL>
-hipError_t launch_up(const DecodeProblem& p, const Geometry& g, size_t lds, hipStream_t stream) {
+hipError_t launch_up(const DecodeProblem& p, const Geometry& g, hipStream_t stream) {
   static OccCache cache;
-  return launch_product(k_decode_up<MX, WHOLE, PL>, cache, p, g, lds, stream);
+  return launch_product(k_decode_up<MX, WHOLE, PL>, cache, p, g, stream);
 }
 // the gate and the up-projection
 template <bool MX, bool WHOLE>
 hipError_t launch_gate_and_up(const DecodeProblem& p, hipStream_t stream) {
-  size_t lds;
-  const Geometry g = geometry(p, p.F, p.d, p.F_shared, p.d, 2, MX, lds);
+  const Geometry g = geometry(p, p.F, p.d, p.F_shared, p.d, 2, MX);
   const int64_t blocks = (int64_t)decode_entries(p.T, p.top_k, p.E_local) * g.tiles;
   // The gates in every workgroup, where there is a wave per token and a lane per slot, and all workgroups are on the chip
   // at once and start with them: one token through 128 experts of 2048 x 768 in bf16 32.8 us a call against 36.0, through
   // 48 of 7168 x 2048 in 4 bits with a shared expert 50.8 against 56.5; four tokens the same either way.
   if (p.T <= kOwnTokens && p.T * p.top_k <= kOwnSlots && p.E <= 512 && blocks <= 4 * cu_count()) {
-    static_assert(kRedBytes >= kOwnTokens * 64 * 8 * 4, "keys of 512 experts in a launch's LDS");
-    return p.E <= 64 ? launch_up<MX, WHOLE, 1>(p, g, lds, stream) : p.E <= 128 ? launch_up<MX, WHOLE, 2>(p, g, lds, stream)
-           : p.E <= 256 ? launch_up<MX, WHOLE, 4>(p, g, lds, stream) : launch_up<MX, WHOLE, 8>(p, g, lds, stream);
+    static_assert(kDecodeRedBytes >= kOwnTokens * 64 * 8 * 4, "keys of 512 experts in a launch's LDS");
+    return p.E <= 64 ? launch_up<MX, WHOLE, 1>(p, g, stream) : p.E <= 128 ? launch_up<MX, WHOLE, 2>(p, g, stream)
+           : p.E <= 256 ? launch_up<MX, WHOLE, 4>(p, g, stream) : launch_up<MX, WHOLE, 8>(p, g, stream);
   }
   const hipError_t e = p.E <= 64 ? launch_decode_gate<1>(p, stream) : p.E <= 128 ? launch_decode_gate<2>(p, stream)
                        : p.E <= 256 ? launch_decode_gate<4>(p, stream) : p.E <= 512 ? launch_decode_gate<8>(p, stream)
                                                                                     : launch_decode_gate<16>(p, stream);
-  return e != hipSuccess ? e : launch_up<MX, WHOLE, 0>(p, g, lds, stream);
+  return e != hipSuccess ? e : launch_up<MX, WHOLE, 0>(p, g, stream);
 }
 template <bool MX, bool WHOLE>
 hipError_t launch_down(const DecodeProblem& p, hipStream_t stream) {
   static OccCache cache;
-  size_t lds;
-  const Geometry g = geometry(p, p.d, p.F, p.d, p.F_shared, 1, MX, lds);
-  return launch_product(k_decode_down<MX, WHOLE>, cache, p, g, lds, stream);
+  const Geometry g = geometry(p, p.d, p.F, p.d, p.F_shared, 1, MX);
+  return launch_product(k_decode_down<MX, WHOLE>, cache, p, g, stream);
 }
 
 template <bool MX>
