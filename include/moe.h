@@ -397,7 +397,8 @@ int moe_mx_grouped_ffn(const moe_shape_t* shape, int format, const void* x_q, co
  *   residual NULL: h is x itself, nothing is added and h must be NULL.  Otherwise h is required; it
  *                  may be x's or residual's own buffer.
  *   y, or y_q and y_scales together, may be NULL (not wanted), not all three; rstd may be NULL.
- *   eps >= 0 and finite.  A row of zeros with eps = 0 gives NaN.
+ *   eps >= 0 and finite.  A row of zeros with eps = 0 gives NaN.  rstd is a float32: with eps = 0 it is
+ *   infinite for rows whose root mean square is below 2^-128 (y is not; the backward's dx is).
  * No output but h may overlap an input.  d a multiple of 8 up to 2^31 - 32, of 32 where y_q is given;
  * 0 <= rows < 2^31. */
 int moe_add_rmsnorm(int64_t rows, int32_t d, float eps, const void* x, const void* residual, const void* gamma,

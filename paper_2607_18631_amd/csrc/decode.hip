@@ -24,11 +24,11 @@
 // than the weights did: 385 us against 210 in the second case below.)  Every load that the compiler sees in
 // the loop is unconditional: behind one that may not have been issued, it has to wait for all of them.
 //
-// Measured: 4 tokens on 8 experts of 4096 x 14336 in 4 bits, top-2, of which 5 to 7 are chosen: 101 - 119 us a call,
-// some 5 TB/s of weights; 64 tokens on 48 of 384 experts of 7168 x 2048 in 4 bits, top-8, and a shared expert: 210 us,
-// 4.1 TB/s (up 104 - 111 us, down 77 - 82, gate 13, logits 9.5, combine 4.5); one token, 128 experts of 2048 x 768 in
-// bf16, top-8: 33 us, of which the weights' stream is 16 at the rate of a copy and the four launches that wait for each
-// other the rest.
+// Measured: 4 tokens on 8 experts of 4096 x 14336 in 4 bits, top-2, of which 5 to 7 are chosen: 94 - 114 us a call,
+// some 5 TB/s of weights; 64 tokens on 48 of 384 experts of 7168 x 2048 in 4 bits, top-8, and a shared expert: 194 - 208 us,
+// 4.1 - 4.4 TB/s (up 104 - 114 us, down 78 - 85, gate 14, logits 10, combine 4.7); one token, 128 experts of 2048 x 768 in
+// bf16, top-8: 30 us (logits 4.4, up 16.9, down 8.0, combine 3.8), of which the weights' stream is 14 at the rate of a read
+// and the four launches that wait for each other the rest.
 #include "common.hpp"
 #include "decode_geometry.hpp"
 #include "gate_device.hpp"
@@ -558,8 +558,9 @@ hipError_t launch_gate_and_up(const DecodeProblem& p, hipStream_t stream) {
   const Geometry g = geometry(p, p.F, p.d, p.F_shared, p.d, 2, MX);
   const int64_t blocks = (int64_t)decode_entries(p.T, p.top_k, p.E_local) * g.tiles;
   // The gates in every workgroup, where there is a wave per token and a lane per slot, and all workgroups are on the chip
-  // at once and start with them: one token through 128 experts of 2048 x 768 in bf16 32.8 us a call against 36.0, through
-  // 48 of 7168 x 2048 in 4 bits with a shared expert 50.8 against 56.5; four tokens the same either way.
+  // at once and start with them: one token through 128 experts of 2048 x 768 in bf16 29.9 us a captured call against 32.5, in 4
+  // bits 22.8 against 25.3, through 48 of 384 of 7168 x 2048 in 4 bits with a shared expert 32.7 against 39.0; four tokens 62.3
+  // against 63.6, 34.1 against 35.5, and the same either way.
   if (p.T <= kOwnTokens && p.T * p.top_k <= kOwnSlots && p.E <= 512 && blocks <= 4 * cu_count()) {
     static_assert(kDecodeRedBytes >= kOwnTokens * 64 * 8 * 4, "keys of 512 experts in a launch's LDS");
     return p.E <= 64 ? launch_up<MX, WHOLE, 1>(p, g, stream) : p.E <= 128 ? launch_up<MX, WHOLE, 2>(p, g, stream)

@@ -13,9 +13,9 @@
 // each workgroup leaves one row of partial sums, which a second kernel adds in a fixed order (a single workgroup writes
 // dgamma itself).
 //
-// All of them are bound by memory.  Measured (bytes read and written over the time; a large copy runs at 4.8 TB/s):
-// conversion of 131072 x 7168 to e2m1 and back 839 us, 5.1 TB/s; norm of 8192 x 7168 with both results 98 us, 5.4 TB/s;
-// norm and backward of 16384 x 2048 106 us, 4.4 TB/s, of 3001 x 2040 26 - 27 us (three launches), 3.3 TB/s; one row 4.5 us,
+// All of them are bound by memory.  Measured (bytes read and written over the time; a large copy runs at 5.1 - 5.5 TB/s):
+// conversion of 131072 x 7168 to e2m1 and back 841 us, 5.1 TB/s; norm of 8192 x 7168 with both results 98 us, 5.4 TB/s;
+// norm and backward of 16384 x 2048 106 us, 4.4 TB/s, of 3001 x 2040 26.5 us (three launches), 3.2 TB/s; one row 4.5 us,
 // a launch.
 #include "common.hpp"
 #include "kernels.hpp"

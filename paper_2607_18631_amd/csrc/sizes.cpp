@@ -62,10 +62,14 @@ int decode_logits_splits(int /*E*/, int d) {
 }
 
 // Norm backward: every workgroup leaves one row of partial sums of dgamma.  A workgroup of four waves takes 4 short rows
-// at once, or one long row.  Few rows go to one workgroup, which needs no second launch (7 rows of 640 13.6 us forward and
-// backward against 16.3); up to 256 workgroups each has one such round (1000 rows of 7168 31 us against 48 with 16 rows a
-// workgroup, 100 of them 16 against 35, 1000 of 2048 16 against 20); then 16 rows, up to four workgroups per compute unit
-// of an MI355X.
+// at once, or one long row.  Few rows go to one workgroup, which needs no second launch; up to 256 workgroups each has one
+// such round; then 16 rows, up to four workgroups per compute unit of an MI355X.  Forward and backward captured in a graph,
+// us a step for numbers of workgroups, the rule's marked:
+//   7 rows of 640   *1 6.4, 2 7.6                      100 of 7168     7 25.7, 50 12.5, *100 11.9
+//   16 of 2048      *1 11.3, 4 9.9                     1000 of 7168    63 37.6, 128 25.9, *256 22.8, 512 23.7
+//   17 of 2048      1 12.1, 2 11.9, *5 10.0            8192 of 7168    256 116, *512 103 - 110, 1024 115
+//   1000 of 2048    63 16.6, 125 14.8, *250 14.8       16384 of 2048   256 59.0, 512 60.6, *1024 65.8, 2048 75
+//   3001 of 2040    188 22.0, *256 19.6, 512 21.0      100000 of 512   512 103, *1024 93.7, 2048 103
 int add_norm_bwd_parts(int64_t rows, int d) {
   const bool is_short = d <= 2048;
   if (rows <= (is_short ? 16 : 2)) return 1;
